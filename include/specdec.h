@@ -339,6 +339,77 @@ int specdec_get_counters(specdec_ctx* ctx, int32_t* counters, void* stream);
 int specdec_quantize_rows(specdec_ctx* ctx, const void* w, int64_t N, int64_t K, void* codes, float* scale,
                                void* stream);
 
+/* ---- operators on tensors of the caller's ------------------------------------------------
+ * Attention over a cache, drawing of tokens and moves of cached rows as calls of their own, for caches and logits that the caller
+ * holds.  Stateless, as specdec_quantize_rows: ctx only receives the error text.  Lengths, masks, settings and indices are read on the
+ * device: values that make no sense are not refused but have the meaning given below, and never cause an access out of bounds. */
+typedef enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1, SPECDEC_F16 = 2 } specdec_dtype;
+
+/* Attention of the rows of drafted trees over a cache.  k, v hold `capacity` rows of every sequence: cached[b] cached ones, behind
+ * them those of the sequence's own rows (row i at cached[b] + i, stored by the caller beforehand).  Row t sees all cached rows and
+ * those of its sequence's rows i whose bit i of visible[b][t] is set:
+ *   out[b][t][h] = sum_s p_s v[b][s][g],  p = softmax over the s it sees of scale * (q[b][t][h] . k[b][s][g]),  g = h / (n_heads / n_kv_heads).
+ * Scores, softmax statistics and sums are fp32; weights are rounded to the element type before they multiply values.  A row that sees
+ * nothing is zeros.  Keys and values that a row does not see do not reach it, whatever they hold. */
+typedef struct {
+  int32_t dtype;                 /* of q, k, v, out: SPECDEC_BF16 or SPECDEC_F16 */
+  int32_t batch;                 /* sequences, at most 65535 */
+  int32_t rows;                  /* rows of a sequence at most, 1 .. 64 (1: decoding of single tokens) */
+  int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads, at most 1024 */
+  int32_t head_dim;              /* 64 or 128 */
+  int32_t capacity;
+  float scale;
+  /* elements between two sequences, rows and heads, multiples of 8, not negative (0: shared); a head's values are consecutive */
+  int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+} specdec_tree_attn_desc;
+/* Bytes of (device) workspace that the call needs, 256-byte aligned; its contents do not matter before or after.  Calls that may
+ * overlap, replays of captured ones among them, need one each. */
+int specdec_tree_attention_bytes(specdec_ctx* ctx, const specdec_tree_attn_desc* desc, size_t* out);
+/* q [batch, rows, n_heads], k / v [batch, capacity, n_kv_heads], out as q, in the strides of desc, 16-byte aligned.
+ * cached int32 [batch]; where it is negative or leaves no room for the sequence's rows, these see nothing.
+ * visible uint64 [batch, rows] (specdec_tree_visible), bits of rows there are not ignored; null: a chain, row t sees rows 0 .. t.
+ * n_rows int32 [batch], rows there are of each sequence (clamped to 0 .. rows); null: all.  The others' out is left as it is. */
+int specdec_tree_attention(specdec_ctx* ctx, const specdec_tree_attn_desc* desc, const void* q, const void* k, const void* v,
+                           const int32_t* cached, const uint64_t* visible, const int32_t* n_rows, void* out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+/* Masks of trees of n drafts (0 <= n <= 63) behind a root: parent int32 [B, n], parent[b][i - 1] in [0, i) the row that row i
+ * (1 .. n) hangs on, row 0 the root -> visible uint64 [B, n + 1].  A row with any other parent (-1, say, in trees of fewer drafts)
+ * is left out, and so are the rows below it: mask 0, seen by none. */
+int specdec_tree_visible(specdec_ctx* ctx, const int32_t* parent, int32_t B, int32_t n, uint64_t* visible, void* stream);
+
+/* One token per row of logits, drawn with the random number u[row] in [0, 1) that the caller brings.
+ * logits [rows, vocab] of the given type, row_stride elements apart, any alignment of the type's own; 1 <= vocab <= 2^24.
+ * Weights are exp((x - max x) / temperature).  In the order of falling logits, equal ones in the order of the vocabulary:
+ *   top_k   the first top_k tokens stay (<= 0: all),
+ *   top_p   of these the first ones, as long as the weights before one sum to less than top_p of them all (>= 1 or NaN: all),
+ *   min_p   of these those whose weight is at least min_p of the largest (NaN: all);
+ * the first token always stays.  token = the first one, in the order of the vocabulary, at which the sum of the weights that stay exceeds
+ * u of their total; logprob (nullable) = the logarithm of its share of that total.  Temperature 0 (or less, or NaN): the largest logit,
+ * lowest index first, logprob 0.  Logits of -inf and NaN are never drawn; +inf outweigh all else; a row without a logit above -inf has token -1
+ * and logprob -inf.  Settings are fp32 (top_k: int32) [rows], null: temperature 1, the others off.
+ * Sums are whole numbers, weights rounded to nearest multiples of 2^-38 of the largest: the same call gives the same tokens. */
+int specdec_sample(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                   const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                   int32_t* token, float* logprob, void* stream);
+
+/* Keys / values as slabs of rows, one per layer, sequence and head, k and v laid out alike. */
+typedef struct {
+  int32_t layers, heads, capacity;   /* layers * heads at most 32767 */
+  int32_t row_bytes;                 /* of a head's row, consecutive; a multiple of 16 */
+  int64_t layer_stride, seq_stride, head_stride, row_stride; /* bytes, multiples of 16, not negative */
+} specdec_cache_desc;
+/* Sequences go on as copies of others, in place: sequence b (< B) gets the first len[src[b]] rows of sequence src[b], in every layer
+ * and head, as they were before the call (src may permute and repeat).  src int32 [B] in [0, n_src), len int32 [n_src] (cut to
+ * the capacity).  Sequences with src[b] = b or outside of the range, and rows behind the copied ones, are left as they are.
+ * B, n_src at most 4096.  v may be null. */
+int specdec_fork_cache(specdec_ctx* ctx, const specdec_cache_desc* desc, void* k, void* v, int32_t B, const int32_t* src,
+                       int32_t n_src, const int32_t* len, void* stream);
+/* Rows move within their sequences, in place: row first[b] + i gets what row first[b] + path[b][i] held before the call, i < count[b]
+ * (the accepted path of a tree, behind the cached rows).  path int32 [B, n], n at most 64, count int32 [B] (at most n),
+ * row_bytes at most 512.  Moves from or to a row outside of [0, capacity) are left out.  B at most 65535.  v may be null. */
+int specdec_compact_cache(specdec_ctx* ctx, const specdec_cache_desc* desc, void* k, void* v, int32_t B, const int32_t* first,
+                          const int32_t* path, int32_t n, const int32_t* count, void* stream);
+
 /* ---- timing of one kernel kind ----------------------------------------------------------- */
 /* While a kind is selected every launch of that kernel is timed by a pair of HIP events on the launch
  * stream (up to 4096 launches between two reads; later ones are not recorded): for the GEMM and attention

@@ -35,6 +35,7 @@ SPECDEC_OPT_FP8_WEIGHTS = 4
 SPECDEC_OPT_FP8_CROSS_KV = 5
 SPECDEC_OPT_WIDE_VOCAB_TILES = 6
 SPECDEC_OPT_GIVE_UP_WAITS = 7
+SPECDEC_F32, SPECDEC_BF16, SPECDEC_F16 = 0, 1, 2
 
 
 class specdec_model_desc(C.Structure):
@@ -44,6 +45,16 @@ class specdec_model_desc(C.Structure):
 
 class specdec_limits(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("max_batch", "k_max", "max_src", "max_tgt")]
+
+
+class specdec_tree_attn_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "batch", "rows", "n_heads", "n_kv_heads", "head_dim", "capacity")] + [
+        ("scale", C.c_float)] + [(n, C.c_int64 * 3) for n in ("q_stride", "k_stride", "v_stride", "out_stride")]
+
+
+class specdec_cache_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layers", "heads", "capacity", "row_bytes")] + [
+        (n, C.c_int64) for n in ("layer_stride", "seq_stride", "head_stride", "row_stride")]
 
 
 EXPORTS = {
@@ -85,6 +96,12 @@ EXPORTS = {
     "specdec_get_cache": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "specdec_get_row_stats": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "specdec_get_memory": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
+    "specdec_tree_attention_bytes": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]),
+    "specdec_tree_attention": (C.c_int, [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]),
+    "specdec_tree_visible": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
+    "specdec_sample": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32, C.c_int64] + [C.c_void_p] * 8),
+    "specdec_fork_cache": (C.c_int, [C.c_void_p] * 4 + [C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "specdec_compact_cache": (C.c_int, [C.c_void_p] * 4 + [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
 }
 
 _lib = None
@@ -297,6 +314,131 @@ def specdec_get_memory(ctx, role: int, memory):
 
 def specdec_get_row_stats(ctx, stats):
     _check(ctx, lib().specdec_get_row_stats(ctx, _ptr(stats), _stream()))
+
+
+# ------------------------------------------------------------------------ operators on the caller's tensors
+def _dtype(t, *allowed) -> int:
+    import torch
+    code = {torch.float32: SPECDEC_F32, torch.bfloat16: SPECDEC_BF16, torch.float16: SPECDEC_F16}.get(t.dtype, -1)
+    if code not in allowed:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"tensors of {t.dtype} are not supported here")
+    return code
+
+
+def _on_gpu(*tensors):
+    """The tensors' storage is on the current GPU, on whose current stream the work goes."""
+    import torch
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != dev):
+            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"a tensor is on {t.device}, not on the current GPU")
+
+
+def _ints(name: str, t, shape, of="int32"):
+    """Device pointer of a contiguous tensor of this shape and type (None -> NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or str(t.dtype) != "torch." + of or not t.is_contiguous():
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: contiguous {of} {list(shape)} expected, not {t.dtype} {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _strided(name: str, t, shape):
+    if tuple(t.shape) != shape or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: {list(shape)} with consecutive last values expected, not {list(t.shape)}, {t.stride()}")
+    return t.data_ptr()
+
+
+def tree_attn_desc(q, k, v, out, scale: float) -> specdec_tree_attn_desc:
+    """Sizes and strides of q, out [B, rows, heads, dim] and k, v [B, kv heads, capacity, dim] (views of any strides, last values consecutive)."""
+    B, T, H, dh = q.shape
+    _, Hkv, cap, _ = k.shape
+    for name, t, shape in (("q", q, (B, T, H, dh)), ("k", k, (B, Hkv, cap, dh)), ("v", v, (B, Hkv, cap, dh)), ("out", out, (B, T, H, dh))):
+        _strided(name, t, shape)
+        if t.dtype != q.dtype:
+            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name} is {t.dtype}, q {q.dtype}")
+    d = specdec_tree_attn_desc(_dtype(q, SPECDEC_BF16, SPECDEC_F16), B, T, H, Hkv, dh, cap, scale)
+    for name, t, dims in (("q_stride", q, (0, 1, 2)), ("k_stride", k, (0, 2, 1)), ("v_stride", v, (0, 2, 1)), ("out_stride", out, (0, 1, 2))):
+        # (a dimension of one has no stride: whatever the tensor says)
+        setattr(d, name, (C.c_int64 * 3)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in dims]))
+    d._shapes = (tuple(q.shape), tuple(k.shape), (B,), (B, T))
+    return d
+
+
+def specdec_tree_attention_bytes(ctx, desc: specdec_tree_attn_desc) -> int:
+    n = C.c_size_t()
+    _check(ctx, lib().specdec_tree_attention_bytes(ctx, C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def specdec_tree_attention(ctx, desc, q, k, v, cached, visible, n_rows, out, workspace):
+    """desc: tree_attn_desc of tensors of these sizes and strides.  visible: int64 [B, rows] (bit masks) or None; n_rows: int32 [B] or None."""
+    q_shape, k_shape, per_seq, per_row = desc._shapes
+    _on_gpu(q, k, v, cached, visible, n_rows, out, workspace)
+    _check(ctx, lib().specdec_tree_attention(
+        ctx, C.byref(desc), _strided("q", q, q_shape), _strided("k", k, k_shape), _strided("v", v, k_shape), _ints("cached", cached, per_seq),
+        _ints("visible", visible, per_row, "int64"), _ints("n_rows", n_rows, per_seq), _strided("out", out, q_shape), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+
+
+def specdec_tree_visible(ctx, parent, visible):
+    """parent int32 [B, n] -> visible int64 [B, n + 1]."""
+    B, n = parent.shape
+    _on_gpu(parent, visible)
+    _check(ctx, lib().specdec_tree_visible(ctx, _ints("parent", parent, (B, n)), B, n, _ints("visible", visible, (B, n + 1), "int64"), _stream()))
+
+
+def specdec_sample(ctx, logits, temperature, top_k, top_p, min_p, u, token, logprob=None):
+    """logits [rows, vocab] (rows of any stride); the settings [rows] or None."""
+    rows, vocab = logits.shape
+    _on_gpu(logits, temperature, top_k, top_p, min_p, u, token, logprob)
+    n = (rows,)
+    _check(ctx, lib().specdec_sample(
+        ctx, _strided("logits", logits, (rows, vocab)), _dtype(logits, SPECDEC_F32, SPECDEC_BF16, SPECDEC_F16), rows, vocab,
+        logits.stride(0) if rows > 1 else 0, _ints("temperature", temperature, n, "float32"), _ints("top_k", top_k, n),
+        _ints("top_p", top_p, n, "float32"), _ints("min_p", min_p, n, "float32"), _ints("u", u, n, "float32"), _ints("token", token, n),
+        _ints("logprob", logprob, n, "float32"), _stream()))
+
+
+def cache_desc(k, v=None) -> specdec_cache_desc:
+    """Sizes and strides of k (and v, laid out alike) [layers, sequences, heads, rows, values] (views of any strides, last values consecutive)."""
+    layers, B, heads, cap, dh = k.shape
+    _strided("k", k, (layers, B, heads, cap, dh))
+    if v is not None and (v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype):
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, "k and v are laid out differently")
+    n = k.element_size()
+    strides = [k.stride(i) * n if k.shape[i] > 1 else 0 for i in (0, 1, 2, 3)]
+    d = specdec_cache_desc(layers, heads, cap, dh * n, *strides)
+    d._shape, d._stride, d._dtype = tuple(k.shape), k.stride(), k.dtype
+    return d
+
+
+def _slabs(desc, *caches):
+    for t in caches:
+        if t is not None and (tuple(t.shape) != desc._shape or t.stride() != desc._stride or t.dtype != desc._dtype):
+            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, "the cache is not laid out as its description says")
+    return [None if t is None else t.data_ptr() for t in caches]
+
+
+def specdec_fork_cache(ctx, desc, k, v, src, length):
+    """desc: cache_desc of k (and v).  src int32 [B], B at most the cache's sequences; length int32 [sequences that src names]."""
+    _on_gpu(k, v, src, length)
+    kp, vp = _slabs(desc, k, v)
+    B, n = src.numel(), length.numel()
+    if max(B, n) > desc._shape[1]:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{B} sequences from {n} in a cache of {desc._shape[1]}")
+    _check(ctx, lib().specdec_fork_cache(ctx, C.byref(desc), kp, vp, B, _ints("src", src, (B,)), n, _ints("length", length, (n,)), _stream()))
+
+
+def specdec_compact_cache(ctx, desc, k, v, first, path, count):
+    """desc: cache_desc of k (and v).  path int32 [B, n], first and count int32 [B]."""
+    _on_gpu(k, v, first, path, count)
+    kp, vp = _slabs(desc, k, v)
+    B, n = path.shape
+    if B > desc._shape[1]:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{B} sequences in a cache of {desc._shape[1]}")
+    _check(ctx, lib().specdec_compact_cache(ctx, C.byref(desc), kp, vp, B, _ints("first", first, (B,)), _ints("path", path, (B, n)), n,
+                                            _ints("count", count, (B,)), _stream()))
 
 
 # ------------------------------------------------------------------------ device memory holder

@@ -1649,6 +1649,130 @@ int specdec_quantize_rows(specdec_ctx* c, const void* w, int64_t N, int64_t K, v
   return SPECDEC_OK;
 }
 
+// ---- operators on tensors of the caller's ----
+}  // extern "C"
+
+namespace {
+
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int attn_args(specdec_ctx* c, const specdec_tree_attn_desc* d, sd::TreeAttnArgs* a) {
+  if (!c) return SPECDEC_ERR_INVALID_ARG;
+  if (!d) return fail(c, SPECDEC_ERR_INVALID_ARG, "null desc");
+  if (d->dtype != SPECDEC_BF16 && d->dtype != SPECDEC_F16) return fail(c, SPECDEC_ERR_INVALID_ARG, "dtype %d (SPECDEC_BF16 or SPECDEC_F16)", d->dtype);
+  if (d->batch < 1 || d->batch > 65535) return fail(c, SPECDEC_ERR_INVALID_ARG, "batch = %d outside [1, 65535]", d->batch);
+  if (d->rows < 1 || d->rows > 64) return fail(c, SPECDEC_ERR_INVALID_ARG, "rows = %d outside [1, 64]", d->rows);
+  if (d->n_kv_heads < 1 || d->n_heads < 1 || d->n_heads > 1024 || d->n_heads % d->n_kv_heads)
+    return fail(c, SPECDEC_ERR_INVALID_ARG, "n_heads = %d, n_kv_heads = %d", d->n_heads, d->n_kv_heads);
+  if (d->head_dim != 64 && d->head_dim != 128) return fail(c, SPECDEC_ERR_INVALID_ARG, "head_dim = %d (64 or 128)", d->head_dim);
+  if (d->capacity < 1 || d->capacity > (1 << 30)) return fail(c, SPECDEC_ERR_INVALID_ARG, "capacity = %d", d->capacity);
+  if (!std::isfinite(d->scale)) return fail(c, SPECDEC_ERR_INVALID_ARG, "scale is not finite");
+  const int64_t* strides[4] = {d->q_stride, d->k_stride, d->v_stride, d->out_stride};
+  for (const int64_t* s : strides)
+    for (int i = 0; i < 3; ++i)
+      if (s[i] < 0 || s[i] % 8 || s[i] > (int64_t(1) << 40)) return fail(c, SPECDEC_ERR_INVALID_ARG, "stride %lld: not a multiple of 8, negative or too large", (long long)s[i]);
+  const int64_t many[3] = {d->batch, d->rows, d->n_heads};
+  for (int i = 0; i < 3; ++i)
+    if (many[i] > 1 && d->out_stride[i] < d->head_dim) return fail(c, SPECDEC_ERR_INVALID_ARG, "rows of out overlap");
+  *a = sd::TreeAttnArgs{};
+  for (int i = 0; i < 3; ++i) { a->q_s[i] = d->q_stride[i]; a->k_s[i] = d->k_stride[i]; a->v_s[i] = d->v_stride[i]; a->o_s[i] = d->out_stride[i]; }
+  a->scale = d->scale;
+  a->B = d->batch; a->T = d->rows; a->H = d->n_heads; a->Hkv = d->n_kv_heads; a->dh = d->head_dim; a->cap = d->capacity;
+  a->f16 = d->dtype == SPECDEC_F16;
+  return SPECDEC_OK;
+}
+
+int slab_args(specdec_ctx* c, const specdec_cache_desc* d, void* k, void* v, sd::CacheSlabs* s) {
+  if (!c) return SPECDEC_ERR_INVALID_ARG;
+  if (!d || !k) return fail(c, SPECDEC_ERR_INVALID_ARG, "null desc/k");
+  if (d->layers < 1 || d->heads < 1 || (int64_t)d->layers * d->heads > 32767) return fail(c, SPECDEC_ERR_INVALID_ARG, "layers = %d, heads = %d", d->layers, d->heads);
+  if (d->capacity < 1 || d->capacity > (1 << 30)) return fail(c, SPECDEC_ERR_INVALID_ARG, "capacity = %d", d->capacity);
+  if (d->row_bytes < 16 || d->row_bytes % 16 || d->row_bytes > 65536) return fail(c, SPECDEC_ERR_INVALID_ARG, "row_bytes = %d: not a multiple of 16 up to 65536", d->row_bytes);
+  for (int64_t s : {d->layer_stride, d->seq_stride, d->head_stride, d->row_stride})
+    if (s < 0 || s % 16 || s > (int64_t(1) << 42)) return fail(c, SPECDEC_ERR_INVALID_ARG, "stride %lld: not a multiple of 16, negative or too large", (long long)s);
+  if (d->capacity > 1 && d->row_stride < d->row_bytes) return fail(c, SPECDEC_ERR_INVALID_ARG, "rows overlap");
+  if (!aligned(k, 16) || !aligned(v, 16)) return fail(c, SPECDEC_ERR_INVALID_ARG, "cache not 16-byte aligned");
+  *s = sd::CacheSlabs{k, v, d->layers, d->heads, d->capacity, d->row_bytes, d->layer_stride, d->seq_stride, d->head_stride, d->row_stride};
+  return SPECDEC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int specdec_tree_attention_bytes(specdec_ctx* c, const specdec_tree_attn_desc* d, size_t* out) {
+  sd::TreeAttnArgs a;
+  const int rc = attn_args(c, d, &a);
+  if (rc) return rc;
+  if (!out) return fail(c, SPECDEC_ERR_INVALID_ARG, "null out");
+  *out = sd::tree_attn_bytes(a);
+  return SPECDEC_OK;
+}
+
+int specdec_tree_attention(specdec_ctx* c, const specdec_tree_attn_desc* d, const void* q, const void* k, const void* v,
+                           const int32_t* cached, const uint64_t* visible, const int32_t* n_rows, void* out, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  sd::TreeAttnArgs a;
+  const int rc = attn_args(c, d, &a);
+  if (rc) return rc;
+  if (!q || !k || !v || !cached || !out) return fail(c, SPECDEC_ERR_INVALID_ARG, "null q/k/v/cached/out");
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16)) return fail(c, SPECDEC_ERR_INVALID_ARG, "q/k/v/out not 16-byte aligned");
+  const size_t need = sd::tree_attn_bytes(a);
+  if (need > 0 && (!workspace || !aligned(workspace, 256))) return fail(c, SPECDEC_ERR_INVALID_ARG, "workspace null or not 256-byte aligned");
+  if (workspace_bytes < need) return fail(c, SPECDEC_ERR_TOO_LARGE, "workspace too small: %zu bytes of %zu", workspace_bytes, need);
+  a.q = q; a.k = k; a.v = v; a.o = out;
+  a.cached = cached; a.visible = reinterpret_cast<const unsigned long long*>(visible); a.rows = n_rows;
+  a.ws = static_cast<float*>(workspace);
+  HIPCHK(c, sd::tree_attn(S(stream), a));
+  return SPECDEC_OK;
+}
+
+int specdec_tree_visible(specdec_ctx* c, const int32_t* parent, int32_t B, int32_t n, uint64_t* visible, void* stream) {
+  if (!c) return SPECDEC_ERR_INVALID_ARG;
+  if ((!parent && n > 0) || !visible) return fail(c, SPECDEC_ERR_INVALID_ARG, "null parent/visible");
+  if (B < 1 || n < 0 || n > 63) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d, n = %d (0 .. 63)", B, n);
+  HIPCHK(c, sd::tree_visible(S(stream), parent, B, n, reinterpret_cast<unsigned long long*>(visible)));
+  return SPECDEC_OK;
+}
+
+int specdec_sample(specdec_ctx* c, const void* logits, specdec_dtype dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                   const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                   int32_t* token, float* logprob, void* stream) {
+  if (!c) return SPECDEC_ERR_INVALID_ARG;
+  if (!logits || !u || !token) return fail(c, SPECDEC_ERR_INVALID_ARG, "null logits/u/token");
+  if (dtype != SPECDEC_F32 && dtype != SPECDEC_BF16 && dtype != SPECDEC_F16) return fail(c, SPECDEC_ERR_INVALID_ARG, "dtype %d", (int)dtype);
+  if (rows < 0 || vocab < 1 || vocab > (1 << 24)) return fail(c, SPECDEC_ERR_INVALID_ARG, "rows = %d, vocab = %d", rows, vocab);
+  if (row_stride < 0 || row_stride > (int64_t(1) << 40)) return fail(c, SPECDEC_ERR_INVALID_ARG, "row_stride = %lld", (long long)row_stride);
+  if (!aligned(logits, dtype == SPECDEC_F32 ? 4 : 2)) return fail(c, SPECDEC_ERR_INVALID_ARG, "logits not aligned to their type");
+  if (rows == 0) return SPECDEC_OK;
+  sd::SampleArgs a{logits, (int)dtype, rows, vocab, row_stride, temperature, top_k, top_p, min_p, u, token, logprob};
+  HIPCHK(c, sd::sample(S(stream), a));
+  return SPECDEC_OK;
+}
+
+int specdec_fork_cache(specdec_ctx* c, const specdec_cache_desc* d, void* k, void* v, int32_t B, const int32_t* src, int32_t n_src,
+                       const int32_t* len, void* stream) {
+  sd::CacheSlabs s;
+  const int rc = slab_args(c, d, k, v, &s);
+  if (rc) return rc;
+  if (!src || !len) return fail(c, SPECDEC_ERR_INVALID_ARG, "null src/len");
+  if (B < 1 || B > 4096 || n_src < 1 || n_src > 4096) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d, n_src = %d outside [1, 4096]", B, n_src);
+  HIPCHK(c, sd::cache_fork(S(stream), s, B, n_src, src, len));
+  return SPECDEC_OK;
+}
+
+int specdec_compact_cache(specdec_ctx* c, const specdec_cache_desc* d, void* k, void* v, int32_t B, const int32_t* first,
+                          const int32_t* path, int32_t n, const int32_t* count, void* stream) {
+  sd::CacheSlabs s;
+  const int rc = slab_args(c, d, k, v, &s);
+  if (rc) return rc;
+  if (!first || !path || !count) return fail(c, SPECDEC_ERR_INVALID_ARG, "null first/path/count");
+  if (B < 1 || B > 65535 || n < 1 || n > sd::kCompactRows) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d, n = %d (1 .. %d)", B, n, sd::kCompactRows);
+  if (s.row_bytes > sd::kCompactRowBytes) return fail(c, SPECDEC_ERR_INVALID_ARG, "row_bytes = %d exceeds %d", s.row_bytes, sd::kCompactRowBytes);
+  HIPCHK(c, sd::cache_compact(S(stream), s, B, n, first, path, count));
+  return SPECDEC_OK;
+}
+
 int specdec_decoder_way(const specdec_ctx* c) { return c ? static_cast<int>(c->way) : -1; }
 
 int specdec_get_row_stats(specdec_ctx* c, float* stats, void* stream) {

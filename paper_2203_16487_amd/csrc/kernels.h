@@ -418,4 +418,52 @@ struct CacheFlat {
 hipError_t cache_load(hipStream_t st, const SeqState& s, const CacheFlat& a, int B);
 hipError_t cache_read(hipStream_t st, const CacheFlat& a, int B);
 
+
+// ---- tree_attn.hip: attention of the rows of a tree over a cache ----
+// Strides in elements, [sequence, row, head]; a head's dims are consecutive.  Every pointer 16-byte aligned, strides multiples of 8.
+struct TreeAttnArgs {
+  const void *q, *k, *v;
+  void* o;
+  long q_s[3], k_s[3], v_s[3], o_s[3];
+  const int* cached;                   // [B] keys in front of the tree's rows; outside of [0, cap - rows]: the rows see nothing
+  const unsigned long long* visible;   // [B][T] which of the sequence's T rows a row sees (null: those up to itself)
+  const int* rows;                     // [B] rows of a sequence (null: T); the others are neither read nor written
+  float scale;
+  int B, T, H, Hkv, dh, cap;
+  bool f16;                            // else bf16
+  float* ws;                           // tree_attn_bytes
+};
+size_t tree_attn_bytes(const TreeAttnArgs& a);
+hipError_t tree_attn(hipStream_t st, const TreeAttnArgs& a);
+// masks [B][n + 1] of the rows of trees from parents [B][n] (n <= 63)
+hipError_t tree_visible(hipStream_t st, const int* parent, int B, int n, unsigned long long* visible);
+
+// ---- sample.hip: tokens drawn from rows of logits ----
+struct SampleArgs {
+  const void* logits;                  // [rows], row_stride elements apart
+  int dtype;                           // 0 fp32, 1 bf16, 2 fp16
+  int rows, vocab;
+  long row_stride;
+  const float* temperature;            // per row, null: 1; not above 0: the largest logit
+  const int* top_k;                    // null, or not above 0: off
+  const float *top_p, *min_p;          // null: off
+  const float* u;
+  int* token;                          // -1 where no logit is above -inf
+  float* logprob;                      // nullable
+};
+hipError_t sample(hipStream_t st, const SampleArgs& a);
+
+// ---- cache_move.hip: sequences and rows of a cache moved in place ----
+// [layers][sequences][heads] slabs of rows; a row's bytes are consecutive, a multiple of 16 and so aligned.  Strides in bytes.
+struct CacheSlabs {
+  void *k, *v;                         // v nullable
+  int layers, heads, capacity, row_bytes;
+  long layer_s, seq_s, head_s, row_s;
+};
+// slab b < B gets the first ceil(len[src[b]] / per) rows of slab src[b], all slabs at once (src[b] = b or outside of [0, n_src): left as it is)
+hipError_t cache_fork(hipStream_t st, const CacheSlabs& c, int B, int n_src, const int* src, const int* len, int per = 1);
+// row first[b] + i of slab b gets what row first[b] + path[b][i] held, i < min(count[b], n), all rows at once (rows outside of the slab: left)
+hipError_t cache_compact(hipStream_t st, const CacheSlabs& c, int B, int n, const int* first, const int* path, const int* count);
+constexpr int kCompactRows = 64, kCompactRowBytes = 512;   // n and row_bytes at most
+
 }  // namespace sd
