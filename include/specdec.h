@@ -353,7 +353,7 @@ typedef enum { SPECDEC_F32 = 0, SPECDEC_BF16 = 1, SPECDEC_F16 = 2 } specdec_dtyp
  * nothing is zeros.  Keys and values that a row does not see do not reach it, whatever they hold. */
 typedef struct {
   int32_t dtype;                 /* of q, k, v, out: SPECDEC_BF16 or SPECDEC_F16 */
-  int32_t batch;                 /* sequences, at most 65535 */
+  int32_t batch;                 /* sequences, at most 65535, and batch x n_heads at most 2^20 */
   int32_t rows;                  /* rows of a sequence at most, 1 .. 64 (1: decoding of single tokens) */
   int32_t n_heads, n_kv_heads;   /* n_heads a multiple of n_kv_heads, at most 1024 */
   int32_t head_dim;              /* 64 or 128 */

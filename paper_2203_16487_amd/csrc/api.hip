@@ -1664,6 +1664,7 @@ int attn_args(specdec_ctx* c, const specdec_tree_attn_desc* d, sd::TreeAttnArgs*
   if (d->rows < 1 || d->rows > 64) return fail(c, SPECDEC_ERR_INVALID_ARG, "rows = %d outside [1, 64]", d->rows);
   if (d->n_kv_heads < 1 || d->n_heads < 1 || d->n_heads > 1024 || d->n_heads % d->n_kv_heads)
     return fail(c, SPECDEC_ERR_INVALID_ARG, "n_heads = %d, n_kv_heads = %d", d->n_heads, d->n_kv_heads);
+  if ((int64_t)d->batch * d->n_heads > (1 << 20)) return fail(c, SPECDEC_ERR_INVALID_ARG, "batch x n_heads = %lld exceeds 2^20", (long long)d->batch * d->n_heads);
   if (d->head_dim != 64 && d->head_dim != 128) return fail(c, SPECDEC_ERR_INVALID_ARG, "head_dim = %d (64 or 128)", d->head_dim);
   if (d->capacity < 1 || d->capacity > (1 << 30)) return fail(c, SPECDEC_ERR_INVALID_ARG, "capacity = %d", d->capacity);
   if (!std::isfinite(d->scale)) return fail(c, SPECDEC_ERR_INVALID_ARG, "scale is not finite");

@@ -3,81 +3,495 @@
 // Sequence b has n_b cached keys / values and T_b rows of its own, whose keys / values lie behind them, at rows n_b + i of the same
 // arena.  Row t sees every cached key and those rows i whose bit is set in visible[b][t] (a tree: itself and its ancestors):
 //   o[b][t][h] = sum_s p_s v[b][s][h / G],  p = softmax over the visible s of scale * (q[b][t][h] . k[b][s][h / G]),  G = H / Hkv.
+//
+// The G query heads of the T rows that share a key head are the G T columns of one pair of products, so a key and a value are read from
+// memory once for all of them (once per block of 32 RW columns, from L2).  A workgroup takes tiles of KT keys through LDS, two buffers, the
+// next tile's direct loads under way while this one is multiplied; its waves are RW groups of 32 columns times KW parts of a tile's keys.
+// Scores are formed as S^T = K Q^T in 32 x 32 tiles: a lane then holds 16 keys of one column, the running maximum and sum are a lane's own up
+// to one exchange of the wave's halves, and the weights are already the second operand of O^T += V^T P^T (the order in which keys are
+// summed is free, so both operands take the one that S^T has).  V^T comes out of LDS by transposing reads.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 
 namespace sd {
 
-template <class E> struct Pack;
-template <> struct Pack<bf16> { typedef bf16 x8 __attribute__((ext_vector_type(8))); };
-template <> struct Pack<f16> { typedef f16 x8 __attribute__((ext_vector_type(8))); };
+typedef unsigned long long u64;
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-// The simplest form: a wave a (sequence, row, query head), lanes over the head's dims, key after key with a running maximum and sum.
-template <class E, int PER>
-__global__ __launch_bounds__(64) void tree_attn_kernel(TreeAttnArgs a) {
-  const int lane = threadIdx.x, h = blockIdx.x % a.H, t = blockIdx.x / a.H, b = blockIdx.y;
-  const int rows = a.rows ? min(max(a.rows[b], 0), a.T) : a.T;
-  if (t >= rows) return;
-  const int n = a.cached[b];
-  const bool fits = n >= 0 && n <= a.cap - rows;
-  const int hk = h / (a.H / a.Hkv);
-  const E* q = static_cast<const E*>(a.q) + b * a.q_s[0] + t * a.q_s[1] + h * a.q_s[2] + lane * PER;
-  const E* k = static_cast<const E*>(a.k) + b * a.k_s[0] + hk * a.k_s[2] + lane * PER;
-  const E* v = static_cast<const E*>(a.v) + b * a.v_s[0] + hk * a.v_s[2] + lane * PER;
-  E* o = static_cast<E*>(a.o) + b * a.o_s[0] + t * a.o_s[1] + h * a.o_s[2] + lane * PER;
-  const unsigned long long seen = a.visible ? a.visible[(size_t)b * a.T + t] : ~0ull >> (63 - t);
-  float qv[PER], acc[PER], m = kNegInf, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < PER; ++e) { qv[e] = (float)q[e] * a.scale; acc[e] = 0.f; }
-  for (int s = 0; fits && s < n + rows; ++s) {
-    if (s >= n && !(seen >> (s - n) & 1)) continue;
-    float d = 0.f;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) d += qv[e] * (float)k[s * a.k_s[1] + e];
-    d = wave_sum(d);
-    const float m2 = fmaxf(m, d), keep = m == kNegInf ? 0.f : __expf(m - m2), p = d == kNegInf ? 0.f : __expf(d - m2);
-    l = l * keep + p;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = acc[e] * keep + p * (float)v[s * a.v_s[1] + e];
-    m = m2;
+// What differs between the element types.  kLift: weights are stored as 2^kLift exp2(s - max), so that fp16, whose values end at 2^-24,
+// keeps weights down to 2^-38 of the largest: without it 65536 keys of 2^-25 each would be lost.
+template <class E> struct AttnType;
+template <> struct AttnType<bf16> {
+  typedef bf16 x8 __attribute__((ext_vector_type(8)));
+  static constexpr float kLift = 0.f;
+  static constexpr unsigned kExp = 0x7f807f80u, kUnit = 0x00800080u;
+  static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
   }
-#pragma unroll
-  for (int e = 0; e < PER; ++e) o[e] = (E)(l == 0.f ? 0.f : acc[e] / l);   // (nothing seen: zeros)
+};
+template <> struct AttnType<f16> {
+  typedef f16 x8 __attribute__((ext_vector_type(8)));
+  static constexpr float kLift = 14.f;
+  static constexpr unsigned kExp = 0x7c007c00u, kUnit = 0x04000400u;
+  static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
+  }
+};
+
+// How a call is cut: blocks of 32 rw columns, tiles of kt keys; split: the tiles of a column block are dealt out in chunks of a length
+// that gives about `target` workgroups in all, whatever the lengths are (the workgroups work it out: the host does not know them), each
+// leaves its maximum, sum and unnormalised output in a slot of the workspace, and tree_join_kernel adds them up.
+struct TreePlan {
+  int rw, kw, kt, row_blocks, target, slots;
+  bool split;
+};
+constexpr int kSplitTarget = 512;
+static TreePlan tree_plan(const TreeAttnArgs& a) {
+  TreePlan p;
+  const int m = a.H / a.Hkv * a.T;
+  p.rw = m <= 32 ? 1 : m <= 64 ? 2 : 4;
+  p.kw = 4 / p.rw;
+  p.kt = p.rw == 1 ? 128 : 64;
+  p.row_blocks = (m + 32 * p.rw - 1) / (32 * p.rw);
+  p.split = a.cap > 8 * p.kt;
+  p.target = kSplitTarget;
+  const long whole = (long)a.B * a.Hkv * p.row_blocks;
+  p.slots = (int)(p.split ? p.target + whole : whole);
+  return p;
 }
 
-size_t tree_attn_bytes(const TreeAttnArgs&) { return 0; }
+// One sequence: rows there are, tiles, column blocks.
+struct TreeSeq { int n, rows, tiles, blocks; };
+__device__ __forceinline__ TreeSeq tree_seq(const TreeAttnArgs& a, const TreePlan& p, int b) {
+  TreeSeq s;
+  s.rows = a.rows ? min(max(a.rows[b], 0), a.T) : a.T;
+  s.n = a.cached[b];
+  if (s.n < 0 || s.n > a.cap - s.rows) s.n = -1;   // (no room for the rows: they see nothing)
+  s.tiles = s.n < 0 ? 1 : (s.n + s.rows + p.kt - 1) / p.kt;
+  s.blocks = (a.H / a.Hkv * s.rows + 32 * p.rw - 1) / (32 * p.rw);
+  return s;
+}
+
+// Where a workgroup's work lies: chunk `chunk` of `chunks` of `per` tiles, in slot `slot`.
+struct TreeWork { int b, hk, block, chunk, chunks, per, slot; bool none; };
+
+__device__ __forceinline__ int wave_sum_i(int v) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// (every wave for itself: lane i has sequences i, i + 64, ..)
+struct TreeDeal { int per, all; };
+template <class F>
+__device__ __forceinline__ TreeDeal tree_deal(const TreeAttnArgs& a, const TreePlan& p, F seq) {
+  const int lane = threadIdx.x & 63;
+  double total = 0.0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const TreeSeq s = seq(b0 + lane);
+    double t = b0 + lane < a.B ? (double)s.blocks * s.tiles : 0.0;
+    for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+    total += t;
+  }
+  TreeDeal d;
+  d.per = max(1, (int)fmin(ceil(total * a.Hkv / p.target), 1073741824.0));
+  int all = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const TreeSeq s = seq(b0 + lane);
+    all += wave_sum_i(b0 + lane < a.B ? a.Hkv * s.blocks * ((s.tiles + d.per - 1) / d.per) : 0);
+  }
+  d.all = all;
+  return d;
+}
+// Running sums of the workgroups of the sequences: f(first slot of the lane's sequence, its slots, sequence) for 64 of them at a time.
+template <class S, class F>
+__device__ __forceinline__ void tree_slots(const TreeAttnArgs& a, int per, S seq, F f) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const TreeSeq s = seq(b0 + lane);
+    const int mine = b0 + lane < a.B ? a.Hkv * s.blocks * ((s.tiles + per - 1) / per) : 0;
+    int sum = mine;
+    for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(sum, o); if (lane >= o) sum += v; }
+    if (f(before + sum - mine, mine, b0, s)) return;
+    before += __shfl(sum, 63);
+  }
+}
+
+__device__ __forceinline__ TreeWork tree_work(const TreeAttnArgs& a, const TreePlan& p, TreeSeq& s) {
+  TreeWork w;
+  w.none = false;
+  if (!p.split) {
+    int id = blockIdx.x;
+    w.block = id % p.row_blocks; id /= p.row_blocks;
+    w.hk = id % a.Hkv;
+    w.b = id / a.Hkv;
+    w.chunk = 0; w.chunks = 1; w.per = 1 << 30; w.slot = 0;
+    s = tree_seq(a, p, w.b);
+    w.none = w.block >= s.blocks;
+    return w;
+  }
+  const int lane = threadIdx.x & 63;
+  const TreeSeq held = tree_seq(a, p, min(lane, a.B - 1));
+  auto seq = [&](int b) { return a.B <= 64 ? held : tree_seq(a, p, min(b, a.B - 1)); };
+  const TreeDeal d = tree_deal(a, p, seq);
+  // neighbours in slot order, which share keys where a key head has several column blocks, go to one XCD
+  const int each = (d.all + 7) / 8, at = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+  w.none = (int)(blockIdx.x >> 3) >= each || at >= d.all;
+  if (w.none) return w;
+  tree_slots(a, d.per, seq, [&](int first, int mine, int b0, const TreeSeq& q) {
+    const unsigned long long in = __builtin_amdgcn_ballot_w64(at >= first && at < first + mine);
+    if (!in) return false;
+    const int from = __builtin_ctzll(in);
+    w.b = b0 + from;
+    s.n = __shfl(q.n, from); s.rows = __shfl(q.rows, from); s.tiles = __shfl(q.tiles, from); s.blocks = __shfl(q.blocks, from);
+    int rest = at - __shfl(first, from);
+    w.per = d.per;
+    w.chunks = (s.tiles + d.per - 1) / d.per;
+    w.hk = rest / (s.blocks * w.chunks); rest -= w.hk * s.blocks * w.chunks;
+    w.chunk = rest / s.blocks;
+    w.block = rest - w.chunk * s.blocks;
+    w.slot = at;
+    return true;
+  });
+  return w;
+}
+
+#define UNIFORM(x) x = __builtin_amdgcn_readfirstlane(x)
+
+template <class E, int DH, int RW, int KW, int SUB>
+__global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs a, TreePlan p) {
+  typedef AttnType<E> Ty;
+  constexpr int WAVES = RW * KW, KT = 32 * KW * SUB, ROW = DH * 2, CH = DH / 8, TILE = KT * ROW;   // bytes of a key, its 16-byte chunks, bytes of a tile
+  constexpr int RPI = 1024 / ROW, LOADS = TILE / 1024 / WAVES;                                     // keys a load of a wave covers, loads a wave
+  constexpr int ET = DH / 32, JOIN = (DH + 4) * 4;                                                 // bytes of a joined row
+  static_assert(LOADS * WAVES * 1024 == TILE, "");
+  extern __shared__ __align__(1024) char lds[];   // [2 buffers][K, V][TILE]; at the end [WAVES][32][JOIN]
+  TreeSeq s;
+  TreeWork w = tree_work(a, p, s);
+  if (w.none) return;
+  UNIFORM(w.b); UNIFORM(w.hk); UNIFORM(w.block); UNIFORM(w.chunk); UNIFORM(w.chunks); UNIFORM(w.per); UNIFORM(w.slot);
+  UNIFORM(s.n); UNIFORM(s.rows); UNIFORM(s.tiles);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave % RW, wk = wave / RW, col = lane & 31, half = lane >> 5;
+  const int G = a.H / a.Hkv, M = G * s.rows;
+  const int m = (w.block * RW + wr) * 32 + col, t = m / G, head = w.hk * G + m - t * G;   // this lane's column: row t, query head
+  const bool there = m < M;
+
+  // keys of this lane's loads: key i * WAVES * RPI + .. of the tile, 16-byte chunk swizzled so that neither the rows of 32 keys nor
+  // the four keys of a transposing read fall on the same banks
+  const int key0 = wave * RPI + lane / CH, last = s.n + s.rows - 1;
+  auto swz = [](int key) { return DH == 128 ? (key & 3) << 2 | (key >> 2 & 3) : (key >> 1 & 1) << 2 | (key >> 2 & 3); };
+  const char* kb = reinterpret_cast<const char*>(static_cast<const E*>(a.k) + w.b * a.k_s[0] + w.hk * a.k_s[2]);
+  const char* vb = reinterpret_cast<const char*>(static_cast<const E*>(a.v) + w.b * a.v_s[0] + w.hk * a.v_s[2]);
+  const long krow = a.k_s[1] * 2, vrow = a.v_s[1] * 2;
+  auto load_tile = [&](int tile, int buf) {
+    char* dst = lds + buf * 2 * TILE + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int in = key0 + i * WAVES * RPI, key = min(tile * KT + in, last);
+      const int chunk = ((lane % CH) ^ swz(in)) * 16;
+      __builtin_amdgcn_global_load_lds(SD_GLB_PTR(kb + key * krow + chunk), SD_LDS_PTR(dst + i * WAVES * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(SD_GLB_PTR(vb + key * vrow + chunk), SD_LDS_PTR(dst + TILE + i * WAVES * 1024), 16, 0, 0);
+    }
+  };
+  int tile = w.chunk * w.per;
+  const int end = s.n < 0 ? tile : min(s.tiles, tile + w.per);
+  if (tile < end) load_tile(tile, 0);
+
+  s16x8 q[DH / 16];
+  {
+    const E* qp = static_cast<const E*>(a.q) + w.b * a.q_s[0] + (there ? t : 0) * a.q_s[1] + (there ? head : w.hk * G) * a.q_s[2] + half * 8;
+#pragma unroll
+    for (int k = 0; k < DH / 16; ++k) q[k] = *reinterpret_cast<const s16x8*>(qp + k * 16);
+  }
+  u64 seen = 0;
+  if (there) seen = (a.visible ? a.visible[(size_t)w.b * a.T + t] : ~0ull >> (63 - t)) & (~0ull >> (64 - s.rows));
+  const float scale = a.scale * 1.44269504088896f;
+
+  f32x16 acc[ET];
+#pragma unroll
+  for (int e = 0; e < ET; ++e) acc[e] = f32x16{};
+  float top = kNegInf, sum = 0.f;
+  const int g = lane & 15, kkey = col, vkey = 4 * half + g / 4;
+  const int kc = swz(kkey) ^ half, vc = ((lane >> 4 & 1) * 2 + (g >> 1 & 1)) ^ swz(vkey);
+
+  // 32 keys of the tile in buffer buf, from key `first` of it, `key` of the sequence
+  auto step = [&](auto masked, const char* kt, const char* vt, int first, int key) {
+    constexpr bool MASK = decltype(masked)::value;
+    f32x16 st = {};
+#pragma unroll
+    for (int k = 0; k < DH / 16; ++k) {
+      const s16x8 kf = *reinterpret_cast<const s16x8*>(kt + (first + kkey) * ROW + ((kc ^ 2 * k) * 16));
+      st = Ty::mfma(kf, q[k], st);
+    }
+    unsigned window = ~0u;   // which of keys 4 half .. + 31 this column sees
+    if constexpr (MASK) {
+      const int rel = key + 4 * half - s.n;
+      window = rel >= 64 ? 0u : rel >= 0 ? (unsigned)(seen >> rel) : rel <= -32 ? ~0u : (unsigned)(seen << -rel) | ((1u << -rel) - 1);
+    }
+    float x[16], big = kNegInf;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = st[i] * scale;
+      if (MASK && !(window >> (8 * (i >> 2) + (i & 3)) & 1)) x[i] = kNegInf;
+      big = fmaxf(big, x[i]);
+    }
+    big = fmaxf(top, half_max(big));
+    const float base = big == kNegInf ? 0.f : big - Ty::kLift;
+    const float keep = __builtin_amdgcn_exp2f(top == kNegInf ? kNegInf : top - big);
+    float part = 0.f;
+    s16x8 pf[2];
+    typename Ty::x8 pv[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(x[i] - base);
+      part += x[i];
+      pv[i >> 3][i & 7] = (E)x[i];
+    }
+    pf[0] = __builtin_bit_cast(s16x8, pv[0]);
+    pf[1] = __builtin_bit_cast(s16x8, pv[1]);
+    sum = sum * keep + part;
+    if (__builtin_amdgcn_ballot_w64(big != top)) {
+#pragma unroll
+      for (int e = 0; e < ET; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[e][i] *= keep;
+    }
+    top = big;
+    if constexpr (MASK) {
+      // Values that some columns see and others do not: 0 x infinity is not 0.  Where the tree's rows of this tile hold any, products one by one.
+      if (a.T > 1 || a.visible) {
+        unsigned odd = 0;
+#pragma unroll
+        for (int i = 0; i < 32 * ROW / 1024; ++i) {
+          const uint4 v4 = *reinterpret_cast<const uint4*>(vt + first * ROW + i * 1024 + lane * 16);
+          for (unsigned u : {v4.x, v4.y, v4.z, v4.w}) odd |= ((u & Ty::kExp) + Ty::kUnit) & 0x80008000u;
+        }
+        if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int reg = (i >> 3) * 4 + (i & 3), h2 = i >> 2 & 1, row = first + i;
+            const float pi = (float)(E)__shfl(x[reg], col + 32 * h2);
+            const bool sees = __shfl(window, col + 32 * h2) >> (8 * (reg >> 2) + (reg & 3)) & 1;
+            if (sees)
+#pragma unroll
+              for (int e = 0; e < ET; ++e)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                  const int dim = e * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+                  acc[e][r] += pi * (float)*reinterpret_cast<const E*>(vt + row * ROW + ((dim / 8) ^ swz(row)) * 16 + (dim & 7) * 2);
+                }
+          }
+          return;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < ET; ++e) {
+        s16x4 v4[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          v4[r] = lds_tr16(reinterpret_cast<const bf16*>(vt + (first + 16 * k + 8 * r + vkey) * ROW + ((vc ^ 4 * e ^ 2 * r) * 16) + (g & 1) * 8));
+        const s16x8 vf = {v4[0][0], v4[0][1], v4[0][2], v4[0][3], v4[1][0], v4[1][1], v4[1][2], v4[1][3]};
+        acc[e] = Ty::mfma(vf, pf[k], acc[e]);
+      }
+  };
+
+  const bool idle = (w.block * RW + wr) * 32 >= M;   // (a wave without columns: it loads and waits with the others)
+  for (int buf = 0; tile < end; ++tile, buf ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();   // every wave's part of this tile is there, and every wave is done with the buffer loaded next
+    if (tile + 1 < end) load_tile(tile + 1, buf ^ 1);
+    if (idle) continue;
+    const char* kt = lds + buf * 2 * TILE;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const int first = (wk * SUB + u) * 32, key = tile * KT + first;
+      if (key + 32 <= s.n) step(std::false_type{}, kt, kt + TILE, first, key);
+      else if (key < s.n + s.rows) step(std::true_type{}, kt, kt + TILE, first, key);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < ET; ++e) mfma_settle(acc[e]);
+  sum = half_add(sum);
+
+  const bool whole = w.chunks == 1;
+  float* slot = a.ws + (size_t)w.slot * 32 * RW * (DH + 2);   // [columns][DH], [columns] maxima, [columns] sums
+  if constexpr (KW == 1) {
+    if (!there) return;
+    if (whole) {
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      E* o = static_cast<E*>(a.o) + w.b * a.o_s[0] + t * a.o_s[1] + head * a.o_s[2] + 4 * half;
+#pragma unroll
+      for (int e = 0; e < ET; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          typedef E x4 __attribute__((ext_vector_type(4)));
+          x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = (E)(acc[e][r * 4 + i] * f);
+          *reinterpret_cast<x4*>(o + e * 32 + r * 8) = v;
+        }
+    } else {
+      float* o = slot + (size_t)(wr * 32 + col) * DH + 4 * half;
+#pragma unroll
+      for (int e = 0; e < ET; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *reinterpret_cast<f32x4*>(o + e * 32 + r * 8) = f32x4{acc[e][r * 4], acc[e][r * 4 + 1], acc[e][r * 4 + 2], acc[e][r * 4 + 3]};
+      if (half == 0) {
+        slot[32 * RW * DH + wr * 32 + col] = top;
+        slot[32 * RW * (DH + 1) + wr * 32 + col] = sum;
+      }
+    }
+  } else {
+    // the waves of a column join what they have: [wave][column][DH + 4], the last four {maximum, sum}
+    __syncthreads();
+    char* mine = lds + (size_t)(wave * 32 + col) * JOIN;
+#pragma unroll
+    for (int e = 0; e < ET; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4*>(mine + (e * 32 + r * 8 + 4 * half) * 4) = f32x4{acc[e][r * 4], acc[e][r * 4 + 1], acc[e][r * 4 + 2], acc[e][r * 4 + 3]};
+    if (half == 0) *reinterpret_cast<f32x4*>(mine + DH * 4) = f32x4{top, sum, 0.f, 0.f};
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * RW * (DH / 4); i += 64 * WAVES) {
+      const int c = i / (DH / 4), d4 = i - c * (DH / 4), mm = w.block * RW * 32 + c;
+      if (mm >= M) break;
+      const char* part[KW];
+      f32x4 st[KW];
+      float all = kNegInf;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) {
+        part[k] = lds + (size_t)((k * RW + c / 32) * 32 + (c & 31)) * JOIN;
+        st[k] = *reinterpret_cast<const f32x4*>(part[k] + DH * 4);
+        all = fmaxf(all, st[k][0]);
+      }
+      f32x4 o = {};
+      float l = 0.f;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) {
+        const float f = st[k][0] == kNegInf && st[k][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[k][0] - all);
+        l += f * st[k][1];
+        const f32x4 v = *reinterpret_cast<const f32x4*>(part[k] + d4 * 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += f * v[j];
+      }
+      if (whole) {
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const int t2 = mm / G;
+        typedef E x4 __attribute__((ext_vector_type(4)));
+        x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (E)(o[j] * f);
+        *reinterpret_cast<x4*>(static_cast<E*>(a.o) + w.b * a.o_s[0] + t2 * a.o_s[1] + (w.hk * G + mm - t2 * G) * a.o_s[2] + d4 * 4) = v;
+      } else {
+        *reinterpret_cast<f32x4*>(slot + (size_t)c * DH + d4 * 4) = o;
+        if (d4 == 0) { slot[32 * RW * DH + c] = all; slot[32 * RW * (DH + 1) + c] = l; }
+      }
+    }
+  }
+}
+
+// The chunks of a (row, query head) added up: a workgroup each, its waves taking every fourth chunk.
+constexpr int kJoinWaves = 4;
+template <class E, int PER>
+__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeAttnArgs a, TreePlan p) {
+  constexpr int DH = 64 * PER;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.x % a.H, t = blockIdx.x / a.H, b = blockIdx.y;
+  const TreeSeq s = tree_seq(a, p, b);
+  if (t >= s.rows) return;
+  const TreeSeq held = tree_seq(a, p, min(lane, a.B - 1));
+  auto seq = [&](int i) { return a.B <= 64 ? held : tree_seq(a, p, min(i, a.B - 1)); };
+  const TreeDeal d = tree_deal(a, p, seq);
+  const int chunks = (s.tiles + d.per - 1) / d.per;
+  if (chunks == 1) return;   // (written by its workgroup)
+  int first = 0;
+  tree_slots(a, d.per, seq, [&](int at, int, int b0, const TreeSeq&) {
+    if (b < b0 || b >= b0 + 64) return false;
+    first = __shfl(at, b - b0);
+    return true;
+  });
+  const int G = a.H / a.Hkv, m = t * G + h % G, block = m / (32 * p.rw), c = m - block * 32 * p.rw;
+  const size_t cols = 32 * p.rw, step = cols * (DH + 2) * s.blocks;
+  const float* slot = a.ws + ((size_t)first + (size_t)(h / G) * s.blocks * chunks + block) * cols * (DH + 2);
+  float top = kNegInf;
+  for (int i = lane; i < chunks; i += 64) top = fmaxf(top, slot[i * step + cols * DH + c]);
+  top = wave_max(top);
+  float o[PER] = {}, l = 0.f;
+#pragma unroll 4
+  for (int i = wave; i < chunks; i += kJoinWaves) {
+    const float mi = slot[i * step + cols * DH + c], li = slot[i * step + cols * (DH + 1) + c];
+    const float f = mi == kNegInf && li == 0.f ? 0.f : __builtin_amdgcn_exp2f(mi - top);
+    l += f * li;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] += f * slot[i * step + (size_t)c * DH + e * 64 + lane];
+  }
+  __shared__ float part[kJoinWaves][DH + 1];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) part[wave][e * 64 + lane] = o[e];
+  if (lane == 0) part[wave][DH] = l;
+  __syncthreads();
+  if (threadIdx.x >= DH) return;
+  float x = 0.f, y = 0.f;
+  for (int i = 0; i < kJoinWaves; ++i) { x += part[i][threadIdx.x]; y += part[i][DH]; }
+  static_cast<E*>(a.o)[b * a.o_s[0] + t * a.o_s[1] + h * a.o_s[2] + threadIdx.x] = (E)(y == 0.f ? 0.f : x / y);
+}
+
+size_t tree_attn_bytes(const TreeAttnArgs& a) {
+  const TreePlan p = tree_plan(a);
+  return p.split ? (size_t)p.slots * 32 * p.rw * (a.dh + 2) * sizeof(float) : 0;
+}
+
+template <class E, int DH, int RW, int KW, int SUB>
+static hipError_t tree_launch(hipStream_t st, const TreeAttnArgs& a, const TreePlan& p) {
+  constexpr int tiles = 4 * 32 * KW * SUB * DH * 2, join = KW > 1 ? RW * KW * 32 * (DH + 4) * 4 : 0, bytes = tiles > join ? tiles : join;
+  const auto kernel = tree_attn_kernel<E, DH, RW, KW, SUB>;
+  static bool ready[64];   // (of each GPU; setting it twice does no harm)
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (bytes > 65536 && !(dev < 64 && ready[dev])) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    if (dev < 64) ready[dev] = true;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.split ? (p.slots + 7) / 8 * 8 : p.slots)), dim3(64 * RW * KW), bytes, st, a, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || !p.split) return e;
+  hipLaunchKernelGGL((tree_join_kernel<E, DH / 64>), dim3(a.T * a.H, a.B), dim3(64 * kJoinWaves), 0, st, a, p);
+  return hipGetLastError();
+}
+
+template <class E, int DH>
+static hipError_t tree_launch_rows(hipStream_t st, const TreeAttnArgs& a) {
+  const TreePlan p = tree_plan(a);
+  return p.rw == 1 ? tree_launch<E, DH, 1, 4, 1>(st, a, p) : p.rw == 2 ? tree_launch<E, DH, 2, 2, 1>(st, a, p) : tree_launch<E, DH, 4, 1, 2>(st, a, p);
+}
 
 hipError_t tree_attn(hipStream_t st, const TreeAttnArgs& a) {
-  const dim3 grid(a.T * a.H, a.B);
-  if (a.f16) {
-    if (a.dh == 128) hipLaunchKernelGGL((tree_attn_kernel<f16, 2>), grid, dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((tree_attn_kernel<f16, 1>), grid, dim3(64), 0, st, a);
-  } else {
-    if (a.dh == 128) hipLaunchKernelGGL((tree_attn_kernel<bf16, 2>), grid, dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((tree_attn_kernel<bf16, 1>), grid, dim3(64), 0, st, a);
-  }
-  return hipGetLastError();
+  if (a.f16) return a.dh == 128 ? tree_launch_rows<f16, 128>(st, a) : tree_launch_rows<f16, 64>(st, a);
+  return a.dh == 128 ? tree_launch_rows<bf16, 128>(st, a) : tree_launch_rows<bf16, 64>(st, a);
 }
 
 // Masks of a tree from its rows' parents: a wave a sequence.  Row 0 is the root; row i (1 .. n) hangs on row parent[i - 1] < i and sees
 // what that sees and itself.  A row whose parent is none of the rows before it, or has been left out, is left out: mask 0.
-__global__ __launch_bounds__(64) void tree_visible_kernel(const int* __restrict__ parent, int n, unsigned long long* __restrict__ visible) {
-  __shared__ unsigned long long mask[64];
+__global__ __launch_bounds__(64) void tree_visible_kernel(const int* __restrict__ parent, int n, u64* __restrict__ visible) {
+  __shared__ u64 mask[64];
   const int lane = threadIdx.x, b = blockIdx.x;
   const int p = lane >= 1 && lane <= n ? parent[(size_t)b * n + lane - 1] : -1;
-  if (lane == 0) {
-    mask[0] = 1;
-    // (one lane: a row follows its parent)
-  }
-  for (int i = 1; i <= n; ++i) {
+  if (lane == 0) mask[0] = 1;
+  for (int i = 1; i <= n; ++i) {   // (one lane: a row follows its parent)
     const int pi = __builtin_amdgcn_readlane(p, i);
-    __syncthreads();
     if (lane == 0) mask[i] = pi >= 0 && pi < i && mask[pi] ? mask[pi] | 1ull << i : 0ull;
   }
   __syncthreads();
   if (lane <= n) visible[(size_t)b * (n + 1) + lane] = mask[lane];
 }
-hipError_t tree_visible(hipStream_t st, const int* parent, int B, int n, unsigned long long* visible) {
+hipError_t tree_visible(hipStream_t st, const int* parent, int B, int n, u64* visible) {
   hipLaunchKernelGGL(tree_visible_kernel, dim3(B), dim3(64), 0, st, parent, n, visible);
   return hipGetLastError();
 }
