@@ -325,26 +325,32 @@ def _dtype(t, *allowed) -> int:
     return code
 
 
-def _on_gpu(*tensors):
-    """The tensors' storage is on the current GPU, on whose current stream the work goes."""
+def _on_gpu(*tensors) -> int:
+    """The current stream, if the tensors' storage is on its GPU."""
     import torch
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != dev):
-            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"a tensor is on {t.device}, not on the current GPU")
+        if t is not None and not t.is_cuda:
+            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"a tensor is on {t.device}")
+    here = torch.cuda.current_stream()
+    dev = here.device_index
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"a tensor is on {t.device}, the current GPU is {dev}")
+    return here.cuda_stream
 
 
 def _ints(name: str, t, shape, of="int32"):
     """Device pointer of a contiguous tensor of this shape and type (None -> NULL)."""
     if t is None:
         return None
-    if tuple(t.shape) != shape or str(t.dtype) != "torch." + of or not t.is_contiguous():
+    import torch
+    if t.shape != shape or t.dtype is not getattr(torch, of) or not t.is_contiguous():
         raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: contiguous {of} {list(shape)} expected, not {t.dtype} {list(t.shape)}")
     return t.data_ptr()
 
 
 def _strided(name: str, t, shape):
-    if tuple(t.shape) != shape or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if t.shape != shape or (shape[-1] > 1 and t.stride(-1) != 1):
         raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: {list(shape)} with consecutive last values expected, not {list(t.shape)}, {t.stride()}")
     return t.data_ptr()
 
@@ -361,7 +367,7 @@ def tree_attn_desc(q, k, v, out, scale: float) -> specdec_tree_attn_desc:
     for name, t, dims in (("q_stride", q, (0, 1, 2)), ("k_stride", k, (0, 2, 1)), ("v_stride", v, (0, 2, 1)), ("out_stride", out, (0, 1, 2))):
         # (a dimension of one has no stride: whatever the tensor says)
         setattr(d, name, (C.c_int64 * 3)(*[t.stride(i) if t.shape[i] > 1 else 0 for i in dims]))
-    d._shapes = (tuple(q.shape), tuple(k.shape), (B,), (B, T))
+    d._like = [(t.shape, t.stride(), t.dtype) for t in (q, k, v, out)]
     return d
 
 
@@ -371,33 +377,40 @@ def specdec_tree_attention_bytes(ctx, desc: specdec_tree_attn_desc) -> int:
     return n.value
 
 
+def _as_described(name: str, t, like):
+    """Device pointer of a tensor of the sizes, strides and type that a description was made of."""
+    if t.shape != like[0] or t.stride() != like[1] or t.dtype is not like[2]:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: {t.dtype} {list(t.shape)}, {t.stride()} is not what the description was made of")
+    return t.data_ptr()
+
+
 def specdec_tree_attention(ctx, desc, q, k, v, cached, visible, n_rows, out, workspace):
     """desc: tree_attn_desc of tensors of these sizes and strides.  visible: int64 [B, rows] (bit masks) or None; n_rows: int32 [B] or None."""
-    q_shape, k_shape, per_seq, per_row = desc._shapes
-    _on_gpu(q, k, v, cached, visible, n_rows, out, workspace)
+    like, B = desc._like, (desc.batch,)
+    stream = _on_gpu(q, k, v, cached, visible, n_rows, out, workspace)
     _check(ctx, lib().specdec_tree_attention(
-        ctx, C.byref(desc), _strided("q", q, q_shape), _strided("k", k, k_shape), _strided("v", v, k_shape), _ints("cached", cached, per_seq),
-        _ints("visible", visible, per_row, "int64"), _ints("n_rows", n_rows, per_seq), _strided("out", out, q_shape), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+        ctx, C.byref(desc), _as_described("q", q, like[0]), _as_described("k", k, like[1]), _as_described("v", v, like[2]),
+        _ints("cached", cached, B), _ints("visible", visible, (desc.batch, desc.rows), "int64"), _ints("n_rows", n_rows, B),
+        _as_described("out", out, like[3]), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), stream))
 
 
 def specdec_tree_visible(ctx, parent, visible):
     """parent int32 [B, n] -> visible int64 [B, n + 1]."""
     B, n = parent.shape
-    _on_gpu(parent, visible)
-    _check(ctx, lib().specdec_tree_visible(ctx, _ints("parent", parent, (B, n)), B, n, _ints("visible", visible, (B, n + 1), "int64"), _stream()))
+    stream = _on_gpu(parent, visible)
+    _check(ctx, lib().specdec_tree_visible(ctx, _ints("parent", parent, (B, n)), B, n, _ints("visible", visible, (B, n + 1), "int64"), stream))
 
 
 def specdec_sample(ctx, logits, temperature, top_k, top_p, min_p, u, token, logprob=None):
     """logits [rows, vocab] (rows of any stride); the settings [rows] or None."""
     rows, vocab = logits.shape
-    _on_gpu(logits, temperature, top_k, top_p, min_p, u, token, logprob)
+    stream = _on_gpu(logits, temperature, top_k, top_p, min_p, u, token, logprob)
     n = (rows,)
     _check(ctx, lib().specdec_sample(
         ctx, _strided("logits", logits, (rows, vocab)), _dtype(logits, SPECDEC_F32, SPECDEC_BF16, SPECDEC_F16), rows, vocab,
         logits.stride(0) if rows > 1 else 0, _ints("temperature", temperature, n, "float32"), _ints("top_k", top_k, n),
         _ints("top_p", top_p, n, "float32"), _ints("min_p", min_p, n, "float32"), _ints("u", u, n, "float32"), _ints("token", token, n),
-        _ints("logprob", logprob, n, "float32"), _stream()))
+        _ints("logprob", logprob, n, "float32"), stream))
 
 
 def cache_desc(k, v=None) -> specdec_cache_desc:
@@ -408,37 +421,32 @@ def cache_desc(k, v=None) -> specdec_cache_desc:
         raise SpecDecError(SPECDEC_ERR_INVALID_ARG, "k and v are laid out differently")
     n = k.element_size()
     strides = [k.stride(i) * n if k.shape[i] > 1 else 0 for i in (0, 1, 2, 3)]
-    d = specdec_cache_desc(layers, heads, cap, dh * n, *strides)
-    d._shape, d._stride, d._dtype = tuple(k.shape), k.stride(), k.dtype
+    d = specdec_cache_desc(layers, heads, cap, dh * n, strides[0], strides[1], strides[2], strides[3])
+    d._like = (k.shape, k.stride(), k.dtype)
     return d
 
 
-def _slabs(desc, *caches):
-    for t in caches:
-        if t is not None and (tuple(t.shape) != desc._shape or t.stride() != desc._stride or t.dtype != desc._dtype):
-            raise SpecDecError(SPECDEC_ERR_INVALID_ARG, "the cache is not laid out as its description says")
-    return [None if t is None else t.data_ptr() for t in caches]
+def _slabs(desc, k, v, B: int):
+    if B > desc._like[0][1]:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{B} sequences in a cache of {desc._like[0][1]}")
+    return _as_described("k", k, desc._like), None if v is None else _as_described("v", v, desc._like)
 
 
 def specdec_fork_cache(ctx, desc, k, v, src, length):
     """desc: cache_desc of k (and v).  src int32 [B], B at most the cache's sequences; length int32 [sequences that src names]."""
-    _on_gpu(k, v, src, length)
-    kp, vp = _slabs(desc, k, v)
+    stream = _on_gpu(k, v, src, length)
     B, n = src.numel(), length.numel()
-    if max(B, n) > desc._shape[1]:
-        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{B} sequences from {n} in a cache of {desc._shape[1]}")
-    _check(ctx, lib().specdec_fork_cache(ctx, C.byref(desc), kp, vp, B, _ints("src", src, (B,)), n, _ints("length", length, (n,)), _stream()))
+    kp, vp = _slabs(desc, k, v, max(B, n))
+    _check(ctx, lib().specdec_fork_cache(ctx, C.byref(desc), kp, vp, B, _ints("src", src, (B,)), n, _ints("length", length, (n,)), stream))
 
 
 def specdec_compact_cache(ctx, desc, k, v, first, path, count):
     """desc: cache_desc of k (and v).  path int32 [B, n], first and count int32 [B]."""
-    _on_gpu(k, v, first, path, count)
-    kp, vp = _slabs(desc, k, v)
+    stream = _on_gpu(k, v, first, path, count)
     B, n = path.shape
-    if B > desc._shape[1]:
-        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{B} sequences in a cache of {desc._shape[1]}")
+    kp, vp = _slabs(desc, k, v, B)
     _check(ctx, lib().specdec_compact_cache(ctx, C.byref(desc), kp, vp, B, _ints("first", first, (B,)), _ints("path", path, (B, n)), n,
-                                            _ints("count", count, (B,)), _stream()))
+                                            _ints("count", count, (B,)), stream))
 
 
 # ------------------------------------------------------------------------ device memory holder

@@ -129,4 +129,4 @@ def test_binding_refuses_tensors(ctx):
     with pytest.raises(sd.SpecDecError):
         sd.cache_desc(k[None], k.transpose(1, 2).contiguous().transpose(1, 2)[None])
     with pytest.raises(sd.SpecDecError):
-        sd._slabs(sd.cache_desc(k[None]), k[None, :1])
+        sd._slabs(sd.cache_desc(k[None]), k[None, :1], None, 1)
