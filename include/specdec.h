@@ -297,6 +297,29 @@ int specdec_verify_static(specdec_ctx* ctx, const int32_t* draft, int32_t k, int
 int specdec_commit(specdec_ctx* ctx, const int32_t* accept_len, const int32_t* next_token,
                    int32_t* n_active_or_null, void* stream);
 
+/* Verification of a tree of drafts: several continuations of every sequence in one pass.  draft, parent device int32 [B, n],
+ * 0 <= n <= k_max: row 0 is the pending token u_j, row i (1 .. n) draft[b][i - 1] on the row parent[b][i - 1] in [0, i).  A row sees the
+ * cached tokens, its ancestors and itself, at the position that its depth gives it: its logits are those of plain decoding along
+ * its path.  A row with any other parent (-1, in trees of fewer drafts) is left out, with the rows below it; its logits mean nothing.
+ * logits device fp32 [B, n + 1, V].  Separate launches, with the weights that specdec_verify reads for as many rows.  Changes no length. */
+int specdec_verify_tree(specdec_ctx* ctx, const int32_t* draft, const int32_t* parent, int32_t n, float* logits, void* stream);
+
+/* Commit of the latest specdec_verify_tree by one token per row, token device int32 [B, n + 1] (specdec_sample on its logits; with
+ * temperature 0 greedy decoding): from the root on to the row that hangs on the present one and whose draft is the token there (the lowest
+ * of them), as long as there is one; these drafts and the token of the last row are appended, as by specdec_commit, and their keys / values
+ * moved behind the cached ones.  Whatever the drafts are, the tokens committed are drawn from the model's distribution: a draft is
+ * kept only where it is the token drawn.  accept_len, next_token (nullable) device int32 [B]: drafts kept and the token behind them,
+ * -1 / pad_id where keys / values are missing (specdec_verify) or the token of a row reached is outside of the vocabulary (nothing
+ * is committed then), 0 / pad_id for finished sequences.  n_active_or_null: as for specdec_commit. */
+int specdec_commit_tree(specdec_ctx* ctx, const int32_t* token, int32_t* accept_len, int32_t* next_token, int32_t* n_active_or_null,
+                        void* stream);
+
+/* The batch goes on as B sequences (at most max_batch), b as a copy of what sequence src[b] is now (device int32 [B], cut to the present
+ * batch): stream, length, cap, what is cached, cross-attention keys / values, of every bound model.  For several outputs of one input,
+ * or without the sequences that have ended.  Nothing is encoded or prefilled again, and the arenas are used in place.  A verification pass
+ * not yet committed, draft statistics and encoder memories (specdec_get_memory) do not outlive it. */
+int specdec_fork(specdec_ctx* ctx, const int32_t* src, int32_t B, void* stream);
+
 /* Roll sequences back: j_b <- min(j_b, len[b]) (len device int32 [B]); cached lengths are cut
  * to match and a sequence whose j drops below its cap is unfinished again.  Like the
  * rollback inside commit this moves no data: rows beyond j are simply dead. */

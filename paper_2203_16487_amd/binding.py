@@ -96,6 +96,9 @@ EXPORTS = {
     "specdec_get_cache": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "specdec_get_row_stats": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p]),
     "specdec_get_memory": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]),
+    "specdec_verify_tree": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "specdec_commit_tree": (C.c_int, [C.c_void_p] * 6),
+    "specdec_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "specdec_tree_attention_bytes": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]),
     "specdec_tree_attention": (C.c_int, [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]),
     "specdec_tree_visible": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
@@ -274,6 +277,19 @@ def specdec_verify_static(ctx, draft, k: int, beta: int, tau: float, accept_len,
 
 def specdec_commit(ctx, accept_len, next_token, n_active=None):
     _check(ctx, lib().specdec_commit(ctx, _ptr(accept_len), _ptr(next_token), _ptr(n_active), _stream()))
+
+
+def specdec_verify_tree(ctx, draft, parent, logits):
+    """draft, parent int32 [B, n] (None: n = 0); logits fp32 [B, n + 1, V]."""
+    _check(ctx, lib().specdec_verify_tree(ctx, _ptr(draft), _ptr(parent), 0 if draft is None else draft.shape[1], _ptr(logits), _stream()))
+
+
+def specdec_commit_tree(ctx, token, accept_len=None, next_token=None, n_active=None):
+    _check(ctx, lib().specdec_commit_tree(ctx, _ptr(token), _ptr(accept_len), _ptr(next_token), _ptr(n_active), _stream()))
+
+
+def specdec_fork(ctx, src):
+    _check(ctx, lib().specdec_fork(ctx, _ptr(src), src.numel(), _stream()))
 
 
 def specdec_rewind(ctx, length):

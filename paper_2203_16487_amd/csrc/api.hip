@@ -100,6 +100,7 @@ struct Model {
   float* row_stats = nullptr;  // [Rmax][kRowStats]
   float* zd = nullptr;       // [Rmax] logit of the draft each row scores
   bf16* slots = nullptr;     // [Bmax*k_max][d] final hidden states of the drafter's mask slots
+  float* tree_ws = nullptr;  // workspace of the attention of trees (tree_attn_bytes; none for arenas it does not split)
   int* new_rows = nullptr;   // [Bmax] stream rows of the current prefill / draft pass
   // encoder activations, rows = Bmax * Scap
   float* ex = nullptr;
@@ -123,6 +124,7 @@ struct specdec_ctx {
   int B = 0;          // batch of the current begin()
   int max_new = 0;
   int last_T = 0;     // rows per sequence (k + 1) of the latest verify (0: none)
+  int last_tree = 0;  // rows per sequence of the latest pass, if that was one over trees (0: none)
   int last_k_draft = 0;   // k of the latest drafter pass (0: none)
   const float* last_row_stats = nullptr;   // merged row statistics of the latest verify
   // final hidden states of the latest verify: rows [B*T][d], normalised, or still to be normalised with (fin_g, fin_b)
@@ -286,8 +288,26 @@ size_t carve_state(const specdec_ctx* c, void* base, sd::SeqState* out) {
   s.src_len = cv.take<int>(Bm);
   s.last_draft = cv.take<int>(Bm * s.k_max);
   s.scratch = cv.take<int>(8);
+  s.visible = cv.take<unsigned long long>(Bm * (s.k_max + 1));
+  s.path = cv.take<int>(Bm * (s.k_max + 1));
+  s.first = cv.take<int>(Bm);
+  s.count = cv.take<int>(Bm);
+  s.accept = cv.take<int>(Bm);
+  s.next = cv.take<int>(Bm);
+  s.fork = cv.take<int>(Bm);
   if (out) *out = s;
   return (cv.off + 255) & ~size_t(255);
+}
+
+// Self-attention of B trees of T rows over a model's arenas, but for the pointers.
+sd::TreeAttnArgs tree_args(const specdec_ctx* c, int H, int B, int T) {
+  sd::TreeAttnArgs a{};
+  const long d = 64l * H;
+  a.q_s[0] = a.o_s[0] = T * d; a.q_s[1] = a.o_s[1] = d; a.q_s[2] = a.o_s[2] = 64;
+  a.k_s[0] = a.v_s[0] = d * c->Lcap; a.k_s[1] = a.v_s[1] = 64; a.k_s[2] = a.v_s[2] = 64l * c->Lcap;
+  a.scale = 0.125f;
+  a.B = B; a.T = T; a.H = a.Hkv = H; a.dh = 64; a.cap = c->Lcap;
+  return a;
 }
 
 size_t carve_model(const specdec_ctx* c, const specdec_model_desc* d, void* base, Model* m) {
@@ -340,6 +360,7 @@ size_t carve_model(const specdec_ctx* c, const specdec_model_desc* d, void* base
   t.rm.row_start = cv.take<int>(Bm + 1);
   t.slots = cv.take<bf16>(Bm * (size_t)c->lim.k_max * D);
   t.new_rows = cv.take<int>(Bm);
+  t.tree_ws = cv.take<float>(sd::tree_attn_bytes(tree_args(c, d->n_heads, (int)Bm, c->lim.k_max + 1)) / sizeof(float));
   t.pl_err = cv.take<int>(64);
   t.pl_layers = cv.take<sd::PlLayer>((size_t)d->dec_layers * (c->fp8 ? 2 : 1));
   if (sd::persist_supported(d->dec_layers, (int)D, (int)F)) {
@@ -376,7 +397,7 @@ size_t carve_model(const specdec_ctx* c, const specdec_model_desc* d, void* base
     m->lnp[0] = t.lnp[0]; m->lnp[1] = t.lnp[1]; m->fold = t.fold;
     m->x = t.x; m->x2 = t.x2; m->skp = t.skp; m->hx = t.hx; m->w8 = t.w8; m->w8s = t.w8s; m->fold8 = t.fold8; m->xk8 = t.xk8; m->xv8 = t.xv8; m->xks = t.xks; m->xvs = t.xvs; m->xb = t.xb; m->q = t.q; m->att = t.att; m->hid = t.hid;
     m->part = t.part; m->row_stats = t.row_stats; m->zd = t.zd; m->rm = t.rm;
-    m->slots = t.slots; m->new_rows = t.new_rows; m->pl_err = t.pl_err;
+    m->slots = t.slots; m->tree_ws = t.tree_ws; m->new_rows = t.new_rows; m->pl_err = t.pl_err;
     m->pl_layers = t.pl_layers; m->pl_exch = t.pl_exch; m->pl_rows = t.pl_rows; m->room = t.room;
     m->xcd_stream = t.xcd_stream; m->xcd_vecs = t.xcd_vecs;
     m->ex = t.ex; m->exb = t.exb; m->eqkv = t.eqkv; m->eatt = t.eatt; m->ehid = t.ehid;
@@ -405,8 +426,9 @@ inline void cross_fp8(const Model& m, int l, sd::AttnArgs& a) {
 // few (verify passes of at most 32 rows, LayerNorm folded): the projections stream the E4M3 copies if the model has them, and
 // the last sum stays un-normalised in m.x (the small-batch vocabulary kernel normalises it itself); so it does with leave_sum (and
 // LayerNorm folded), for vocab_stats.
+// trees: the rows are those of trees (c->st.visible), T a sequence.
 int decoder_layers(specdec_ctx* c, Model& m, int B, int T, hipStream_t st, bool embedded = false, int slot_k = 0,
-                   bool packed = false, bool kv_only = false, bool few = false, bool leave_sum = false) {
+                   bool packed = false, bool kv_only = false, bool few = false, bool leave_sum = false, bool trees = false) {
   const int R = B * T, D = m.d.d_model, F = m.d.d_ffn, H = m.d.n_heads;
   const int Lcap = c->Lcap, Scap = c->Scap;
   const int* m_real = packed ? m.rm.row_start + B : nullptr;
@@ -446,7 +468,13 @@ int decoder_layers(specdec_ctx* c, Model& m, int B, int T, hipStream_t st, bool 
     a.q_count = m.rm.seq_rows; a.q_off = row_start; a.lim_row = m.rm.row_lim; a.lim_seq = nullptr;
     a.T = T; a.H = H; a.B = B;
     a.key_split = Lcap > 256; a.cap = Lcap;
-    LAUNCH(c, SPECDEC_KIND_ATTN, st, sd::attention(st, a));
+    if (trees) {
+      sd::TreeAttnArgs ta = tree_args(c, H, B, T);
+      ta.q = m.q; ta.k = kc; ta.v = vc; ta.o = m.att; ta.cached = c->st.len; ta.visible = c->st.visible; ta.ws = m.tree_ws;
+      LAUNCH(c, SPECDEC_KIND_ATTN, st, sd::tree_attn(st, ta));
+    } else {
+      LAUNCH(c, SPECDEC_KIND_ATTN, st, sd::attention(st, a));
+    }
     if (fold) {
       LAUNCH(c, SPECDEC_KIND_GEMM_F32, st, sum(m.att, D, W.wo, fd.vo));
       LAUNCH(c, SPECDEC_KIND_GEMM_BF16, st, sd::gemm_ln_bf16(st, m.xb, W.cwq, R, D, D, fd.cq, pend, m.q, D, false, m_real));
@@ -1093,7 +1121,7 @@ int specdec_begin(specdec_ctx* c, int32_t B, int32_t max_new, void* stream) {
                             c->m[1].bound ? c->m[1].pl_err : nullptr, sd::kPlFlags + 2 * sd::kXcdFlags));
   c->B = B;
   c->max_new = max_new;
-  c->last_T = 0;
+  c->last_T = c->last_tree = 0;
   c->last_k_draft = 0;
   c->uncached_ub[0] = 0;
   c->uncached_ub[1] = c->uncached_block = 1;
@@ -1261,7 +1289,7 @@ static void stream_replaced(specdec_ctx* c, int32_t L_max) {
   c->uncached_ub[1] = c->uncached_block = L_max + 1;
   c->short_cache = false;
   c->trusted[0] = c->trusted[1] = false;
-  c->last_T = 0;
+  c->last_T = c->last_tree = 0;
 }
 
 int specdec_set_stream(specdec_ctx* c, const int32_t* tokens, const int32_t* len, int32_t L_max, void* stream) {
@@ -1455,6 +1483,7 @@ int verify_impl(specdec_ctx* c, const int32_t* draft, int32_t k, int32_t beta, f
   LAUNCH(c, SPECDEC_KIND_ACCEPT, st, sd::merge_accept(st, vs.part, vs.zd, n_tiles, vs.row_stats, c->st, B, k, beta, tau, m.d.pad_id,
                                       accept_len, next_token, failed));
   c->last_T = k + 1;
+  c->last_tree = 0;
   c->last_row_stats = vs.row_stats;
   return SPECDEC_OK;
 }
@@ -1532,17 +1561,113 @@ int specdec_draft_heads(specdec_ctx* c, const int32_t* accept_len, int32_t k, in
   return SPECDEC_OK;
 }
 
+// (two at least: a drafter's pass that came to nothing leaves a sequence behind, and a place more than plain steps need lets it catch up)
+static void committed(specdec_ctx* c, int rows, hipStream_t st) {
+  c->uncached_block += std::max(rows, 2);
+  c->uncached_ub[1] += c->lim.k_max + 1;
+  (void)drafter_uncached(c, st);   // (captured?)
+}
+
 int specdec_commit(specdec_ctx* c, const int32_t* accept_len, const int32_t* next_token, int32_t* n_active, void* stream) {
   int rc = check_ready(c, SPECDEC_VERIFIER, false);
   if (rc) return rc;
   if (!accept_len || !next_token) return fail(c, SPECDEC_ERR_INVALID_ARG, "null accept_len/next_token");
   if (c->last_T <= 0) return fail(c, SPECDEC_ERR_BAD_STATE, "specdec_commit without a preceding specdec_verify");
   HIPCHK(c, sd::commit_rows(S(stream), c->st, accept_len, next_token, c->B, c->last_T - 1, c->m[0].d.eos_id, n_active));
-  // (two at least: a drafter's pass that came to nothing leaves a sequence behind, and a place more than plain steps need lets it catch up)
-  c->uncached_block += std::max(c->last_T, 2);
+  committed(c, c->last_T, S(stream));
   c->last_T = 0;
-  c->uncached_ub[1] += c->lim.k_max + 1;
-  (void)drafter_uncached(c, S(stream));   // (captured?)
+  return SPECDEC_OK;
+}
+
+int specdec_verify_tree(specdec_ctx* c, const int32_t* draft, const int32_t* parent, int32_t n, float* logits, void* stream) {
+  int rc = check_ready(c, SPECDEC_VERIFIER, true);
+  if (rc) return rc;
+  if (!logits || (n > 0 && (!draft || !parent))) return fail(c, SPECDEC_ERR_INVALID_ARG, "null draft/parent/logits");
+  if (n < 0) return fail(c, SPECDEC_ERR_INVALID_ARG, "n = %d", n);
+  if (n > c->lim.k_max) return fail(c, SPECDEC_ERR_TOO_LARGE, "n = %d exceeds k_max = %d", n, c->lim.k_max);
+  Model& m = c->m[SPECDEC_VERIFIER];
+  if (c->uncached_ub[0] > 0 && !c->trusted[0]) return fail(c, SPECDEC_ERR_BAD_STATE, "verifier cache does not cover the stream: call specdec_prefill or specdec_load_cache");
+  const int B = c->B, T = n + 1, R = B * T, D = m.d.d_model;
+  hipStream_t st = S(stream);
+  // what a verification pass of as many rows reads: of few the E4M3 copies of the weights, if the model has them
+  const bool small = skinny_ok(c, m, R, T) && !c->no_ln_fold;
+  if (m.fp8 && c->no_ln_fold && skinny_ok(c, m, R, T))
+    return fail(c, SPECDEC_ERR_BAD_STATE, "trees of a model bound with FP8 weights need SPECDEC_OPT_LN_FOLD = 1");
+  if (small && (m.fp8 || m.kv8) && (c->resident || c->sliced))
+    return fail(c, SPECDEC_ERR_BAD_STATE, "a model bound with FP8 weights or FP8 cross keys/values runs small passes on the default kernels only");
+  if (small && !m.skinny_ready) {
+    HIPCHK(c, sd::skinny_init(D));
+    m.skinny_ready = true;
+  }
+  c->last_T = c->last_tree = 0;
+  LAUNCH(c, SPECDEC_KIND_OTHER, st, sd::assemble_embed_tree(st, c->st, m.rm, draft, parent, B, n, m.d.vocab, m.embed, m.pe, m.x, m.xb, D));
+  rc = decoder_layers(c, m, B, T, st, true, 0, false, false, small, !small, true);
+  if (rc) return rc;
+  const bf16 *g = m.dec.back().ln3g, *b = m.dec.back().ln3b;
+  if (small) {
+    const sd::SkSrc fin{2, m.x, g, b, nullptr, nullptr, nullptr, nullptr};
+    LAUNCH(c, SPECDEC_KIND_VOCAB, st, sd::skinny_vocab(st, fin, R, D, m.fp8 ? m.embed8 : sd::SkWeight(m.embed), m.d.vocab, m.rm.row_draft, m.zd, m.part, logits));
+  } else {
+    const sd::VocabLn ln{m.x, g, b, m.xb};
+    LAUNCH(c, SPECDEC_KIND_VOCAB, st, sd::vocab_stats(st, m.xb, m.embed, R, m.d.vocab, D, nullptr, nullptr, m.part, logits, c->wide_vocab, c->no_ln_fold ? nullptr : &ln));
+  }
+  c->last_tree = T;
+  return SPECDEC_OK;
+}
+
+int specdec_commit_tree(specdec_ctx* c, const int32_t* token, int32_t* accept_len, int32_t* next_token, int32_t* n_active, void* stream) {
+  int rc = check_ready(c, SPECDEC_VERIFIER, false);
+  if (rc) return rc;
+  if (!token) return fail(c, SPECDEC_ERR_INVALID_ARG, "null token");
+  if (c->last_tree <= 0) return fail(c, SPECDEC_ERR_BAD_STATE, "specdec_commit_tree without a preceding specdec_verify_tree");
+  const Model& m = c->m[SPECDEC_VERIFIER];
+  hipStream_t st = S(stream);
+  const int T = c->last_tree, B = c->B, H = m.d.n_heads;
+  HIPCHK(c, sd::tree_walk(st, c->st, token, B, T - 1, m.d.vocab, m.d.pad_id, accept_len, next_token));
+  if (T > 1) {
+    const sd::CacheSlabs s{m.kc, m.vc, m.d.dec_layers, H, c->Lcap, 128, (long)m.kv_layer * 2, (long)H * c->Lcap * 128, (long)c->Lcap * 128, 128};
+    HIPCHK(c, sd::cache_compact(st, s, B, T, c->st.first, c->st.path, c->st.count));
+  }
+  HIPCHK(c, sd::commit_rows(st, c->st, c->st.accept, c->st.next, B, T - 1, m.d.eos_id, n_active));
+  committed(c, T, st);
+  c->last_tree = 0;
+  return SPECDEC_OK;
+}
+
+int specdec_fork(specdec_ctx* c, const int32_t* src, int32_t B_new, void* stream) {
+  if (!c) return SPECDEC_ERR_INVALID_ARG;
+  if (!c->state_bound || c->B <= 0) return fail(c, SPECDEC_ERR_BAD_STATE, "begin not called");
+  if (!src) return fail(c, SPECDEC_ERR_INVALID_ARG, "null src");
+  if (B_new < 1) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d", B_new);
+  if (B_new > c->lim.max_batch) return fail(c, SPECDEC_ERR_TOO_LARGE, "B = %d exceeds max_batch = %d", B_new, c->lim.max_batch);
+  hipStream_t st = S(stream);
+  const int B = c->B;
+  HIPCHK(c, sd::fork_src(st, c->st, src, B_new, B));
+  for (int role = 0; role < 2; ++role) {
+    Model& m = c->m[role];
+    if (!m.bound) continue;
+    const int H = m.d.n_heads, L = m.d.dec_layers;
+    // rows of `bytes` for `per` keys each, of an arena of `elem` bytes a value
+    auto fork = [&](void* k, void* v, size_t layer, int cap, int bytes, int per, const int* len) {
+      const long head = (long)cap / per * bytes;
+      const sd::CacheSlabs s{k, v, L, H, cap / per, bytes, (long)layer, H * head, head, bytes};
+      return sd::cache_fork(st, s, B_new, B, c->st.fork, len, per);
+    };
+    HIPCHK(c, fork(m.kc, m.vc, m.kv_layer * 2, c->Lcap, 128, 1, c->st.cached[role]));
+    if (!m.has_memory) continue;
+    const int S = c->Scap;   // (values lie in blocks of 8 keys)
+    HIPCHK(c, fork(m.xk, nullptr, m.xkv_layer * 2, S, 128, 1, c->st.src_len));
+    HIPCHK(c, fork(m.xv, nullptr, m.xkv_layer * 2, S, 1024, 8, c->st.src_len));
+    if (m.kv8) {
+      HIPCHK(c, fork(m.xk8, nullptr, m.xkv_layer, S, 64, 1, c->st.src_len));
+      HIPCHK(c, fork(m.xv8, nullptr, m.xkv_layer, S, 512, 8, c->st.src_len));
+      HIPCHK(c, fork(m.xks, m.xvs, m.xkv_layer / 16, S, 16, 4, c->st.src_len));
+    }
+    m.enc_packed = false;
+  }
+  HIPCHK(c, sd::fork_state(st, c->st, B_new));
+  c->B = B_new;
+  c->last_T = c->last_tree = c->last_k_draft = 0;
   return SPECDEC_OK;
 }
 
@@ -1551,7 +1676,7 @@ int specdec_rewind(specdec_ctx* c, const int32_t* len, void* stream) {
   if (!c->state_bound || c->B <= 0) return fail(c, SPECDEC_ERR_BAD_STATE, "begin not called");
   if (!len) return fail(c, SPECDEC_ERR_INVALID_ARG, "null len");
   HIPCHK(c, sd::rewind_state(S(stream), c->st, len, c->B));
-  c->last_T = 0;
+  c->last_T = c->last_tree = 0;
   return SPECDEC_OK;
 }
 
@@ -1612,7 +1737,7 @@ int specdec_get_memory(specdec_ctx* c, specdec_role role, void* memory, void* st
   if (!memory) return fail(c, SPECDEC_ERR_INVALID_ARG, "null memory");
   Model& m = c->m[role];
   if (m.d.enc_layers == 0 || !m.exb) return fail(c, SPECDEC_ERR_BAD_STATE, "model has no encoder");
-  if (!m.enc_packed) return fail(c, SPECDEC_ERR_BAD_STATE, "the memory in use was supplied by specdec_set_memory, not computed by specdec_encode");
+  if (!m.enc_packed) return fail(c, SPECDEC_ERR_BAD_STATE, "the memory in use was not computed by specdec_encode for the present batch (specdec_set_memory, specdec_fork)");
   HIPCHK(c, sd::unpack_rows(S(stream), m.exb, m.erow_start, c->st.src_len, static_cast<bf16*>(memory), c->B, c->S_cur,
                             m.d.d_model));
   return SPECDEC_OK;

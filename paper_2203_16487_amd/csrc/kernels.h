@@ -345,8 +345,23 @@ struct SeqState {       // device arrays of the bound state buffer, all [max_bat
   int* src_len;
   int* last_draft;      // [max_batch][k_max]
   int* scratch;         // [8] counters since begin: commits, tokens appended, finished sequences, near-tau rows; three words of commit_kernel's
+  // of the latest pass over trees: what its rows see, [max_batch][k_max + 1]
+  unsigned long long* visible;
+  int* path;            // [max_batch][k_max + 1] rows of the tree along which its tokens were accepted
+  int *first, *count, *accept, *next;   // of the same: row of the root, rows of the path (0: nothing to commit), accepted drafts, token behind them
+  int* fork;            // which sequence each one goes on from (fork_src)
   int tok_pitch, k_max;
 };
+// rows of a pass over trees, the root u_j and n drafts: embedded at j + (depth in the tree), keys / values at j + row; also stores the drafts
+// and what each row sees for tree_walk
+hipError_t assemble_embed_tree(hipStream_t st, const SeqState& s, const RowMap& rm, const int* draft, const int* parent, int B, int n, int V,
+                               const bf16* E, const float* pe, float* x, bf16* xb, int d);
+// Along the rows that carry the token drawn on their parent, from the root: s.path / first / count / accept / next, the drafts of the path in order
+// in s.last_draft, accept_len / next_token (nullable) as of a verification pass
+hipError_t tree_walk(hipStream_t st, const SeqState& s, const int* token, int B, int n, int V, int pad_id, int* accept_len, int* next_token);
+// s.fork = src within [0, B); what is kept of a sequence (tokens, lengths, flags) from the sequences that s.fork names, all at once
+hipError_t fork_src(hipStream_t st, const SeqState& s, const int* src, int B_new, int B);
+hipError_t fork_state(hipStream_t st, const SeqState& s, int B_new);
 // rows of a verification pass: [u_j, drafts]; also stores the drafts for commit
 hipError_t assemble_verify(hipStream_t st, const SeqState& s, const RowMap& rm, const int* draft,
                            int B, int k, int V);

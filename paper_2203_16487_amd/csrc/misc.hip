@@ -250,6 +250,144 @@ hipError_t assemble_embed_verify(hipStream_t st, const SeqState& s, const RowMap
   return hipGetLastError();
 }
 
+// ----------------------------------------------------------------------------- tree rows
+// Row 0 of sequence b is u_j, row i >= 1 draft i on the row parent[b][i - 1] < i.  A row sees its ancestors and itself and is embedded as many
+// places behind u_j as it has ancestors; keys and values lie at j + i, whatever the tree.  A row whose chain of parents does not end
+// in the root is left out: mask 0, seen by none.  One block per row.
+__global__ __launch_bounds__(128) void assemble_embed_tree_kernel(SeqState s, RowMap rm, const int* __restrict__ draft, const int* __restrict__ parent,
+                                                                  int n, int V, const bf16* __restrict__ E, const float* __restrict__ pe,
+                                                                  float* __restrict__ x, bf16* __restrict__ xb, int d, float scale) {
+  __shared__ float red[2];
+  __shared__ int up[32];
+  const int idx = blockIdx.x, T = n + 1, b = idx / T, i = idx - b * T, j = s.len[b];
+  if ((int)threadIdx.x < n) up[threadIdx.x + 1] = parent[(size_t)b * n + threadIdx.x];
+  __syncthreads();
+  unsigned seen = 1u << i;
+  for (int r = i; r > 0;) {   // (all threads alike: every step goes to a lower row)
+    const int q = up[r];
+    if (q < 0 || q >= r) { seen = 0; break; }
+    r = q;
+    seen |= 1u << r;
+  }
+  const int depth = seen ? __popc(seen) - 1 : 0;
+  int tok = (i == 0) ? s.tokens[(size_t)b * s.tok_pitch + j] : draft[(size_t)b * n + i - 1];
+  if (threadIdx.x == 0) {
+    rm.row_b[idx] = b;
+    rm.row_pos[idx] = j + i;
+    rm.row_lim[idx] = j + i + 1;
+    rm.row_draft[idx] = -1;
+    s.visible[(size_t)b * T + i] = seen;
+    if (i > 0) s.last_draft[b * s.k_max + i - 1] = tok;
+    if (i == 0) rm.seq_rows[b] = T;
+  }
+  tok = min(max(tok, 0), V - 1);
+  if (threadIdx.x == 0) rm.row_tok[idx] = tok;
+  embed_row(E + (size_t)tok * d, pe + (size_t)(j + depth) * d, x + (size_t)idx * d, xb + (size_t)idx * d, d, scale, threadIdx.x, red);
+}
+hipError_t assemble_embed_tree(hipStream_t st, const SeqState& s, const RowMap& rm, const int* draft, const int* parent, int B, int n, int V,
+                               const bf16* E, const float* pe, float* x, bf16* xb, int d) {
+  hipLaunchKernelGGL(assemble_embed_tree_kernel, dim3(B * (n + 1)), dim3(128), 0, st, s, rm, draft, parent, n, V, E, pe, x, xb, d, sqrtf((float)d));
+  return hipGetLastError();
+}
+
+// A wave a sequence, lane i for row i: the parent of a row is the highest of its ancestors.  From the root on to the lowest row that hangs on
+// the present one and carries the token drawn there, as long as there is one; the token of the last row follows the path.
+__global__ __launch_bounds__(64) void tree_walk_kernel(SeqState s, const int* __restrict__ token, int n, int V, int pad_id, int* __restrict__ accept_len,
+                                                       int* __restrict__ next_token) {
+  const int b = blockIdx.x, i = threadIdx.x, T = n + 1;
+  const bool row = i < T;
+  const unsigned seen = row ? (unsigned)s.visible[(size_t)b * T + i] : 0u;
+  const int tok = row ? token[(size_t)b * T + i] : 0, draft = row && i > 0 ? s.last_draft[b * s.k_max + i - 1] : -1;
+  const int len = s.len[b], cached = s.cached[0][b], finished = s.finished[b];
+  const int parent = seen && i > 0 ? 31 - __builtin_clz(seen ^ 1u << i) : -1;
+  int at = 0, a = 0, path = 0, taken = pad_id;   // lane l: the path's row l, its token
+  bool drawn = true;
+  int t;
+  for (;;) {
+    t = __builtin_amdgcn_readlane(tok, at);
+    drawn = t >= 0 && t < V;
+    const unsigned long long on = __builtin_amdgcn_ballot_w64(parent == at && draft == t);
+    if (!drawn || !on) break;
+    at = __builtin_ctzll(on);   // (above the present row: the walk ends)
+    ++a;
+    if (i == a) { path = at; taken = t; }
+  }
+  // nothing to commit: finished, keys / values missing, nothing drawn on the last row
+  const bool failed = cached < len || !drawn, none = finished || failed;
+  if (i <= a) s.path[(size_t)b * T + i] = path;
+  if (!none && i >= 1 && i <= a) s.last_draft[b * s.k_max + i - 1] = taken;
+  if (i != 0) return;
+  s.first[b] = len;
+  s.count[b] = none ? 0 : a + 1;
+  const int acc = finished ? 0 : failed ? -1 : a, next = none ? pad_id : t;
+  s.accept[b] = acc;
+  s.next[b] = next;
+  if (accept_len) accept_len[b] = acc;
+  if (next_token) next_token[b] = next;
+}
+hipError_t tree_walk(hipStream_t st, const SeqState& s, const int* token, int B, int n, int V, int pad_id, int* accept_len, int* next_token) {
+  hipLaunchKernelGGL(tree_walk_kernel, dim3(B), dim3(64), 0, st, s, token, n, V, pad_id, accept_len, next_token);
+  return hipGetLastError();
+}
+
+// ----------------------------------------------------------------------------- forked sequences
+__global__ void fork_src_kernel(SeqState s, const int* __restrict__ src, int B_new, int B) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b < B_new) s.fork[b] = min(max(src[b], 0), B - 1);
+}
+hipError_t fork_src(hipStream_t st, const SeqState& s, const int* src, int B_new, int B) {
+  hipLaunchKernelGGL(fork_src_kernel, dim3((B_new + 127) / 128), dim3(128), 0, st, s, src, B_new, B);
+  return hipGetLastError();
+}
+// A block has 2^shift consecutive places of the streams in every sequence, the last one the other arrays: what could overwrite a source is
+// the same block's, and all its loads are done before its first store.
+constexpr int kForkWords = 8, kForkArrays = 7;
+__global__ __launch_bounds__(1024) void fork_state_kernel(SeqState s, int B, int shift) {
+  int held[kForkWords], to[kForkWords];
+  if (blockIdx.x + 1 == gridDim.x) {   // (at most 4 x 1024 sequences)
+    int* const one[kForkArrays] = {s.len, s.start, s.cap, s.finished, s.cached[0], s.cached[1], s.src_len};
+    int more[4][kForkArrays];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int b = q * 1024 + (int)threadIdx.x;
+      if (b >= B) continue;
+      const int from = s.fork[b];
+#pragma unroll
+      for (int i = 0; i < kForkArrays; ++i) more[q][i] = one[i][from];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int b = q * 1024 + (int)threadIdx.x;
+      if (b >= B) continue;
+#pragma unroll
+      for (int i = 0; i < kForkArrays; ++i) one[i][b] = more[q][i];
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kForkWords; ++i) {
+    const int u = i * 1024 + (int)threadIdx.x, b = u >> shift, at = ((int)blockIdx.x << shift) + (u & ((1 << shift) - 1));
+    to[i] = -1;
+    if (b >= B || at >= s.tok_pitch) continue;
+    held[i] = s.tokens[(size_t)s.fork[b] * s.tok_pitch + at];
+    to[i] = at;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kForkWords; ++i)
+    if (to[i] >= 0) s.tokens[(size_t)((i * 1024 + (int)threadIdx.x) >> shift) * s.tok_pitch + to[i]] = held[i];
+}
+hipError_t fork_state(hipStream_t st, const SeqState& s, int B_new) {
+  if (B_new > 4096) return hipErrorInvalidValue;
+  int shift = 0;
+  while ((B_new << (shift + 1)) <= 1024 * kForkWords) ++shift;
+  hipLaunchKernelGGL(fork_state_kernel, dim3(((s.tok_pitch + (1 << shift) - 1) >> shift) + 1), dim3(1024), 0, st, s, B_new, shift);
+  return hipGetLastError();
+}
+
 // ----------------------------------------------------------------------------- prefill / draft rows
 // Each sequence owns up to T row slots of the pass.
 // Prefill (n_mask = 0): the next up to T uncached stream tokens, causal.

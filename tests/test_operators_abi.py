@@ -130,3 +130,13 @@ def test_binding_refuses_tensors(ctx):
         sd.cache_desc(k[None], k.transpose(1, 2).contiguous().transpose(1, 2)[None])
     with pytest.raises(sd.SpecDecError):
         sd._slabs(sd.cache_desc(k[None]), k[None, :1], None, 1)
+
+
+def test_call_order_without_a_model(ctx):
+    L = sd.lib()
+    assert L.specdec_verify_tree(ctx, P, P, 1, P, None) == sd.SPECDEC_ERR_BAD_STATE
+    assert L.specdec_commit_tree(ctx, P, None, None, None, None) == sd.SPECDEC_ERR_BAD_STATE
+    assert L.specdec_fork(ctx, P, 1, None) == sd.SPECDEC_ERR_BAD_STATE
+    for call in (lambda: L.specdec_verify_tree(None, P, P, 1, P, None), lambda: L.specdec_commit_tree(None, P, None, None, None, None),
+                 lambda: L.specdec_fork(None, P, 1, None)):
+        assert call() == BAD
