@@ -424,7 +424,7 @@ typedef struct {
 /* Sequences go on as copies of others, in place: sequence b (< B) gets the first len[src[b]] rows of sequence src[b], in every layer
  * and head, as they were before the call (src may permute and repeat).  src int32 [B] in [0, n_src), len int32 [n_src] (cut to
  * the capacity).  Sequences with src[b] = b or outside of the range, and rows behind the copied ones, are left as they are.
- * B, n_src at most 4096.  v may be null. */
+ * B, n_src at most 4096, capacity x heads x row_bytes below 32 GiB.  v may be null. */
 int specdec_fork_cache(specdec_ctx* ctx, const specdec_cache_desc* desc, void* k, void* v, int32_t B, const int32_t* src,
                        int32_t n_src, const int32_t* len, void* stream);
 /* Rows move within their sequences, in place: row first[b] + i gets what row first[b] + path[b][i] held before the call, i < count[b]

@@ -1883,6 +1883,8 @@ int specdec_fork_cache(specdec_ctx* c, const specdec_cache_desc* d, void* k, voi
   if (rc) return rc;
   if (!src || !len) return fail(c, SPECDEC_ERR_INVALID_ARG, "null src/len");
   if (B < 1 || B > 4096 || n_src < 1 || n_src > 4096) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d, n_src = %d outside [1, 4096]", B, n_src);
+  if ((int64_t)s.capacity * (s.row_bytes / 16) * s.heads >= (int64_t)1 << 31)
+    return fail(c, SPECDEC_ERR_TOO_LARGE, "capacity x heads x row_bytes of a layer reaches 32 GiB");
   HIPCHK(c, sd::cache_fork(S(stream), s, B, n_src, src, len));
   return SPECDEC_OK;
 }

@@ -476,7 +476,7 @@ struct CacheSlabs {
   long layer_s, seq_s, head_s, row_s;
 };
 // slab b < B gets the first ceil(len[src[b]] / per) rows of slab src[b], all slabs at once (src[b] = b or outside of [0, n_src): left as it is)
-hipError_t cache_fork(hipStream_t st, const CacheSlabs& c, int B, int n_src, const int* src, const int* len, int per = 1);
+hipError_t cache_fork(hipStream_t st, CacheSlabs c, int B, int n_src, const int* src, const int* len, int per = 1);
 // row first[b] + i of slab b gets what row first[b] + path[b][i] held, i < min(count[b], n), all rows at once (rows outside of the slab: left)
 hipError_t cache_compact(hipStream_t st, const CacheSlabs& c, int B, int n, const int* first, const int* path, const int* count);
 constexpr int kCompactRows = 64, kCompactRowBytes = 512;   // n and row_bytes at most

@@ -97,6 +97,8 @@ def test_cache_moves(ctx):
     for args in ((None, P, 2, P, 2, P), (odd, P, 2, P, 2, P), (P, odd, 2, P, 2, P), (P, P, 0, P, 2, P), (P, P, 4097, P, 2, P), (P, P, 2, None, 2, P),
                  (P, P, 2, P, 0, P), (P, P, 2, P, 4097, P), (P, P, 2, P, 2, None)):
         assert L.specdec_fork_cache(ctx, C.byref(d), *args, None) == BAD, args
+    vast = slabs(capacity=1 << 26, layer_stride=0)
+    assert L.specdec_fork_cache(ctx, C.byref(vast), P, P, 2, P, 2, P, None) == LARGE
     assert L.specdec_fork_cache(ctx, None, P, P, 2, P, 2, P, None) == BAD and L.specdec_fork_cache(None, C.byref(d), P, P, 2, P, 2, P, None) == BAD
     for args in ((None, P, 2, P, P, 3, P), (P, odd, 2, P, P, 3, P), (P, P, 0, P, P, 3, P), (P, P, 65536, P, P, 3, P), (P, P, 2, None, P, 3, P), (P, P, 2, P, None, 3, P),
                  (P, P, 2, P, P, 0, P), (P, P, 2, P, P, 65, P), (P, P, 2, P, P, 3, None)):
