@@ -10,9 +10,9 @@
 // sums are off by 1e-7, tokens at the end weigh 1e-4.)
 //
 // A workgroup a row, which is read once and stays in registers where it fits; every wave owns a consecutive part of it, so that the order
-// of the vocabulary is the order of the waves.  The end of top-k and of top-p is found without sorting: logits are counted (and weighed) in
+// of the vocabulary is the order of the waves.  The end of top-k and of top-p is found without sorting: logits are counted (or weighed) in
 // kBuckets equal steps of max - x over the range in which weights are above zero, and the one step that holds the end is settled
-// among its own tokens.
+// among its own tokens.  Weights are formed where something depends on them: of all tokens only for top-p alone and for a plain draw.
 #include "common.h"
 #include "kernels.h"
 
@@ -43,10 +43,20 @@ __device__ __forceinline__ u64 fixed_exp2(double t) {
   return __builtin_bit_cast(u64, r) & 0xfffffffffffffull;
 }
 
-__device__ __forceinline__ u64 shfl_u64(u64 v, int lane) { return __shfl(v, lane); }
+// Sum over the wave, to every lane (the moves of wave_sum).
+template <int CTRL>
+__device__ __forceinline__ u64 dpp_u64(u64 v) {
+  return (u64)(unsigned)dpp_i<CTRL>((int)(v >> 32)) << 32 | (unsigned)dpp_i<CTRL>((int)v);
+}
+__device__ __forceinline__ u64 lane_u64(u64 v, int lane) {
+  return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
 __device__ __forceinline__ u64 sum_u64(u64 v) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  v += dpp_u64<kDppSwap1>(v);
+  v += dpp_u64<kDppSwap2>(v);
+  v += dpp_u64<kDppHalfMirror>(v);
+  v += dpp_u64<kDppMirror>(v);
+  return lane_u64(v, 0) + lane_u64(v, 16) + lane_u64(v, 32) + lane_u64(v, 48);
 }
 __device__ __forceinline__ u64 scan_u64(u64 v) {   // inclusive, over the lanes
   const int lane = threadIdx.x & 63;
@@ -54,141 +64,156 @@ __device__ __forceinline__ u64 scan_u64(u64 v) {   // inclusive, over the lanes
   return v;
 }
 
-// PER values a lane in registers; 0: read again for every pass.
-template <class E, int WAVES, int PER>
+// HOLD 16-byte pieces a lane in registers; 0: read again for every pass.
+template <class E, int WAVES, int HOLD>
 __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
-  constexpr int VEC = 16 / sizeof(E), HOLD = PER / VEC > 0 ? PER / VEC : 1, THREADS = 64 * WAVES, EACH = kBuckets / THREADS;
+  constexpr int VEC = 16 / sizeof(E), THREADS = 64 * WAVES, EACH = kBuckets / THREADS;
   typedef E Vec __attribute__((ext_vector_type(VEC)));
-  __shared__ unsigned cnt[kBuckets];
-  __shared__ u64 mass[kBuckets];
+  typedef unsigned Raw __attribute__((ext_vector_type(4)));
+  __shared__ u64 mass[kBuckets];      // (of counts, where the end of top-k is looked for)
   __shared__ float list[kList];
   __shared__ u64 list_w[kList];
   __shared__ u64 red[2][WAVES];
   __shared__ unsigned list_n;
-  __shared__ struct { u64 over_mass, w; float value; unsigned over, equal; int bucket, index; } end;
+  __shared__ struct { u64 over, w; float value; unsigned equal; int bucket, index; } end;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x, V = a.vocab;
 
   // the row in 16-byte pieces of `VEC` tokens that start before it where it is not aligned; a wave's are consecutive
   const E* x0 = static_cast<const E*>(a.logits) + row * a.row_stride;
   const int shift = (int)((reinterpret_cast<uintptr_t>(x0) & 15) / sizeof(E));
   const int rounds = (V + shift + THREADS * VEC - 1) / (THREADS * VEC), first = wave * rounds * 64 * VEC - shift;
-  auto load = [&](int r, float (&v)[VEC]) {
+  auto load = [&](int r) {
     const int i = first + (r * 64 + lane) * VEC;
-    if (i >= 0 && i + VEC <= V) {
-      const Vec p = *reinterpret_cast<const Vec*>(x0 + i);
+    if (i >= 0 && i + VEC <= V) return *reinterpret_cast<const Raw*>(x0 + i);
+    Vec v;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] = (float)p[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] = i + e >= 0 && i + e < V ? (float)x0[i + e] : kNegInf;
-    }
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) v[e] = v[e] == v[e] ? v[e] : kNegInf;
+    for (int e = 0; e < VEC; ++e) v[e] = i + e >= 0 && i + e < V ? x0[i + e] : (E)kNegInf;
+    return __builtin_bit_cast(Raw, v);
   };
-  float held[HOLD][VEC];
-  if constexpr (PER > 0) {
+  Raw held[HOLD > 0 ? HOLD : 1];
+  if constexpr (HOLD > 0) {
 #pragma unroll
     for (int r = 0; r < HOLD; ++r)
-      if (r < rounds) load(r, held[r]);
+      if (r < rounds) held[r] = load(r);
   }
-  bool inf_top = false;
-  auto get = [&](int r, float (&v)[VEC]) {   // (re-read)
-    load(r, v);
+  float top = kNegInf, low = -kNegInf;
+  bool inf_top = false;   // only the infinite ones count: as zeros among -inf
+  auto values = [&](Raw raw, float (&v)[VEC]) {
+    const Vec p = __builtin_bit_cast(Vec, raw);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      v[e] = (float)p[e];
+      v[e] = v[e] == v[e] ? v[e] : kNegInf;
+    }
     if (inf_top)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[e] = v[e] == -kNegInf ? 0.f : kNegInf;
   };
-  // f(round, the lane's values)
+  // f(round, the lane's values) for every round
   auto all = [&](auto f) {
-    if constexpr (PER > 0) {
+    float v[VEC];
+    if constexpr (HOLD > 0) {
 #pragma unroll
       for (int r = 0; r < HOLD; ++r) {
-        // (nothing that is formed of the values outlives its pass, and rounds are not mixed: both would take more registers than there are)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) asm volatile("" : "+v"(held[r][e]));
-        if (r < rounds) f(r, held[r]);
+        asm volatile("" : "+v"(held[r]));   // (nothing formed of the values outlives its pass, and rounds are not mixed: it would not fit the registers)
+        if (r < rounds) { values(held[r], v); f(r, v); }
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      for (int r = 0; r < rounds; ++r) { float v[VEC]; get(r, v); f(r, v); }
+      Raw next = load(0);
+      for (int r = 0; r < rounds; ++r) {
+        const Raw now = next;
+        if (r + 1 < rounds) next = load(r + 1);
+        values(now, v);
+        f(r, v);
+      }
     }
   };
-  auto block_sum = [&](u64 v, u64 w, u64& sv, u64& sw) {   // both sums to everyone
+  // the same in few instructions, where it is seldom done
+  auto again = [&](auto f) {
+    float v[VEC];
+#pragma unroll 1
+    for (int r = 0; r < rounds; ++r) { values(load(r), v); f(r, v); }
+  };
+  auto block_sum = [&](u64 v) {   // to everyone
     v = sum_u64(v);
-    w = sum_u64(w);
     __syncthreads();
-    if (lane == 0) { red[0][wave] = v; red[1][wave] = w; }
+    if (lane == 0) red[0][wave] = v;
     __syncthreads();
-    sv = sw = 0;
+    u64 s = 0;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) { sv += red[0][i]; sw += red[1][i]; }
+    for (int i = 0; i < WAVES; ++i) s += red[0][i];
+    return s;
+  };
+  auto block_range = [&](float& hi, float& lo) {
+    hi = wave_max(hi);
+    lo = -wave_max(-lo);
+    __syncthreads();
+    if (lane == 0) red[0][wave] = (u64)__builtin_bit_cast(unsigned, hi) << 32 | __builtin_bit_cast(unsigned, lo);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      hi = fmaxf(hi, __builtin_bit_cast(float, (unsigned)(red[0][i] >> 32)));
+      lo = fminf(lo, __builtin_bit_cast(float, (unsigned)red[0][i]));
+    }
   };
 
-  float top = kNegInf, low = -kNegInf;
+  const float temperature = a.temperature ? a.temperature[row] : 1.f, p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f;
+  const int k = a.top_k ? a.top_k[row] : 0;
   all([&](int, float (&v)[VEC]) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) { top = fmaxf(top, v[e]); low = fminf(low, v[e] == kNegInf ? -kNegInf : v[e]); }
   });
-  top = wave_max(top);
-  low = -wave_max(-low);
-  if (lane == 0) red[0][wave] = (u64)__builtin_bit_cast(unsigned, top) << 32 | __builtin_bit_cast(unsigned, low);
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
-    top = fmaxf(top, __builtin_bit_cast(float, (unsigned)(red[0][i] >> 32)));
-    low = fminf(low, __builtin_bit_cast(float, (unsigned)red[0][i]));
-  }
+  block_range(top, low);
   if (top == kNegInf) {   // nothing to draw from
     if (tid == 0) { a.token[row] = -1; if (a.logprob) a.logprob[row] = kNegInf; }
     return;
   }
-  if (top == -kNegInf) {   // only the infinite ones count: as zeros among -inf
-    inf_top = true;
-    top = low = 0.f;
-    if constexpr (PER > 0) {
-#pragma unroll
-      for (int r = 0; r < HOLD; ++r)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) held[r][e] = held[r][e] == -kNegInf ? 0.f : kNegInf;
-    }
-  }
+  if (top == -kNegInf) { inf_top = true; top = low = 0.f; }
 
-  const float temperature = a.temperature ? a.temperature[row] : 1.f, p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f;
-  const int k = a.top_k ? a.top_k[row] : 0;
   const bool alone = !(temperature > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;   // the first token is all that stays
   const double inv_t = 1.0 / (double)temperature, per_x = fmax(inv_t * 1.44269504088896340736, 1e-300);
-  auto weight = [&](float x) {
-    const u64 w = fixed_exp2(((double)x - (double)top) * per_x);
-    __builtin_amdgcn_sched_barrier(0);
-    return w;
-  };
+  auto weight = [&](float x) { return fixed_exp2(((double)x - (double)top) * per_x); };
   const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * kOne) : 0;
+  // below floor_0 nothing weighs anything, below floor_x not `least`, by margins far beyond the rounding of these lines
+  auto floor_of = [&](float nats) { return top - 1.0001f * temperature * (nats + 1e-4f) - 1e-6f * fabsf(top); };
+  const float floor_0 = floor_of(27.1f), floor_x = least > 0 ? floor_of(0.6931472f * (38.f - __builtin_amdgcn_logf((float)least))) : floor_0;
 
-  // the f-th token, in the order of the vocabulary, that a wave's `mine`(x, index) counts add up to: its index; called by one wave
-  auto find = [&](u64 target, auto mine, float& value) {
-    int found = -1;
-    auto look = [&](int r, float (&v)[VEC]) {
-      if (found >= 0) return;
-      const int i0 = first + (r * 64 + lane) * VEC;
-      u64 m[VEC], s = 0;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) { m[e] = mine(v[e], i0 + e); s += m[e]; }
-      const u64 upto = scan_u64(s), total = shfl_u64(upto, 63);
-      if (target >= total) { target -= total; return; }
-      const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > target));
-      u64 left = target - (upto - s);
-      int at = -1;
-      float val = 0.f;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        if (at < 0 && left < m[e]) { at = i0 + e; val = v[e]; }
-        else left -= m[e];
-      }
-      found = __shfl(at, who);
-      value = __shfl(val, who);
+  // the first token, in the order of the vocabulary, at which the wave's sum of mine(value, index) exceeds `target`, which all of it does; sum(r): the
+  // lane's part of round r.  Called by one wave.
+  auto find = [&](u64 target, auto sum, auto mine, float& value) {
+    u64 upto = 0, s = 0;
+    int r = 0;
+    auto one = [&](int q) {
+      const u64 t = sum(q), total = sum_u64(t);
+      if (target < total) { r = q; s = t; return true; }
+      target -= total;
+      return false;
     };
-    all(look);
-    return found;
+    if constexpr (HOLD > 0) {
+      bool got = false;
+#pragma unroll
+      for (int q = 0; q < HOLD; ++q)
+        if (q < rounds && !got) got = one(q);
+    } else {
+      while (!one(r)) ++r;
+    }
+    upto = scan_u64(s);
+    const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > target));
+    float v[VEC];
+    values(load(r), v);
+    const int i0 = first + (r * 64 + lane) * VEC;
+    u64 left = target - (upto - s);
+    int at = -1;
+    float val = 0.f;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const u64 m = mine(v[e], i0 + e);
+      if (at < 0 && left < m) { at = i0 + e; val = v[e]; }
+      else left -= m;
+    }
+    value = __shfl(val, who);
+    return __shfl(at, who);
   };
 
   // the cut: tokens above it stay, and those equal to it up to an index
@@ -199,165 +224,151 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
   if (by_k || by_p) {
     const float range = fminf(27.1f * temperature, (top - low) * 1.001f);   // (2^-39 = exp(-27.03))
     const float steps = (float)(kBuckets - 1) / range;
+    const float floor_k = by_p ? floor_0 : floor_x;   // (what min-p drops counts for top-p)
     auto bucket = [&](float x) {
       const float d = top - x;
       return d > 0.f ? (int)fminf(d * steps, (float)(kBuckets - 1)) : 0;
     };
-    for (int i = tid; i < kBuckets; i += THREADS) { cnt[i] = 0; mass[i] = 0; }
-    if (tid == 0) list_n = 0;
-    __syncthreads();
-    // (by top-p alone: what weighs less than half of (1 - p) / V cannot reach its end)
-    const u64 light = by_p && !by_k ? (u64)(0.5 * (1.0 - (double)p) / V * kOne) : 0;
-    u64 sum = 0, Z, dummy;
-    all([&](int, float (&v)[VEC]) {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const int b = bucket(v[e]);
-        if (by_p) {
-          const u64 w = weight(v[e]);
-          sum += w;
-          if (w > light) atomicAdd(&mass[b], w);
-          if (by_k && w > 0) atomicAdd(&cnt[b], 1u);
-        } else if (b < kBuckets - 1) {   // (the last step: weights of zero)
-          atomicAdd(&cnt[b], 1u);
-        }
-      }
-    });
-    if (by_p) block_sum(sum, 0, Z, dummy);
-    else __syncthreads();
-    // the step in which the running count reaches `need_n`, or the running weight `need_w`; false: none does
-    auto locate = [&](u64 need_n, u64 need_w) {
-      u64 n = 0, w = 0;
-#pragma unroll
-      for (int i = 0; i < EACH; ++i) { n += cnt[tid * EACH + i]; w += mass[tid * EACH + i]; }
-      const u64 un = scan_u64(n), uw = scan_u64(w);
+    auto clear = [&] {
       __syncthreads();
-      if (lane == 63) { red[0][wave] = un; red[1][wave] = uw; }
-      if (tid == 0) end.bucket = -1;
+      for (int i = tid; i < kBuckets; i += THREADS) mass[i] = 0;
       __syncthreads();
-      u64 bn = un - n, bw = uw - w;
-      for (int i = 0; i < wave; ++i) { bn += red[0][i]; bw += red[1][i]; }
-      if (bn < need_n && bw < need_w && (bn + n >= need_n || bw + w >= need_w)) {
+    };
+    // the step in which the running sum reaches `need`; false: none does
+    auto locate = [&](u64 need) {
+      u64 n = 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) n += mass[tid * EACH + i];
+      const u64 un = scan_u64(n);
+      __syncthreads();
+      if (lane == 63) red[0][wave] = un;
+      if (tid == 0) { end.bucket = -1; list_n = 0; }
+      __syncthreads();
+      u64 bn = un - n;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) bn += i < wave ? red[0][i] : 0;
+      if (bn < need && bn + n >= need) {
+#pragma unroll 1
         for (int i = 0; i < EACH; ++i) {
-          const u64 cn = cnt[tid * EACH + i], cw = mass[tid * EACH + i];
-          if (bn + cn >= need_n || bw + cw >= need_w) { end.bucket = tid * EACH + i; end.over = (unsigned)bn; end.over_mass = bw; break; }
-          bn += cn; bw += cw;
+          const u64 cn = mass[tid * EACH + i];
+          if (bn + cn >= need) { end.bucket = tid * EACH + i; end.over = bn; break; }
+          bn += cn;
         }
       }
       __syncthreads();
       return end.bucket >= 0;
     };
-    // settles the end within that step: value, what is above it, how many equal it
-    auto settle = [&](u64 need_n, u64 need_w) {
+    // settles the end within that step: value, the sum of what is above it, how many equal it; each token counts one or its weight
+    auto settle = [&](u64 need, bool weighed) {
       const int B = end.bucket;
-      const u64 over = end.over, over_mass = end.over_mass;
-      __syncthreads();
-      if (tid == 0) list_n = 0;
-      __syncthreads();
+      const u64 over = end.over;
       all([&](int, float (&v)[VEC]) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (v[e] > kNegInf && bucket(v[e]) == B) {
+          if (v[e] >= floor_k && bucket(v[e]) == B) {
             const unsigned at = atomicAdd(&list_n, 1u);
-            if (at < kList) { list[at] = v[e]; list_w[at] = weight(v[e]); }
+            if (at < kList) list[at] = v[e];
           }
       });
       __syncthreads();
       const int n = (int)list_n;
       if (n <= kList) {
+        for (int i = tid; i < n; i += THREADS) list_w[i] = weighed ? weight(list[i]) : 1;
+        __syncthreads();
         for (int i = tid; i < n; i += THREADS) {
           const float x = list[i];
-          u64 cn = over, cw = over_mass;
+          u64 c = over;
           unsigned same = 0;
           for (int j = 0; j < n; ++j) {
             const float y = list[j];
-            if (y > x) { ++cn; cw += list_w[j]; }
+            if (y > x) c += list_w[j];
             same += y == x;
           }
           const u64 w = list_w[i];
-          if (cn < need_n && cw < need_w && (cn + same >= need_n || cw + same * w >= need_w)) {   // (every thread of this value: the same)
-            end.value = x; end.over = (unsigned)cn; end.over_mass = cw; end.equal = same; end.w = w;
-          }
+          if (c < need && c + same * w >= need) { end.value = x; end.over = c; end.equal = same; end.w = w; }   // (every thread of this value: the same)
         }
         __syncthreads();
         return;
       }
       // too many tokens in one step (equal ones, or logits far closer than the temperature): by halves of the keys between its ends
       float hi = kNegInf, lo = -kNegInf;
-      all([&](int, float (&v)[VEC]) {
+      again([&](int, float (&v)[VEC]) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (v[e] > kNegInf && bucket(v[e]) == B) { hi = fmaxf(hi, v[e]); lo = fminf(lo, v[e]); }
       });
-      hi = wave_max(hi);
-      lo = -wave_max(-lo);
-      __syncthreads();
-      if (lane == 0) red[0][wave] = (u64)__builtin_bit_cast(unsigned, hi) << 32 | __builtin_bit_cast(unsigned, lo);
-      __syncthreads();
-      for (int i = 0; i < WAVES; ++i) {
-        hi = fmaxf(hi, __builtin_bit_cast(float, (unsigned)(red[0][i] >> 32)));
-        lo = fminf(lo, __builtin_bit_cast(float, (unsigned)red[0][i]));
-      }
-      auto above = [&](float x, u64& cn, u64& cw) {
-        u64 c = 0, w = 0;
-        all([&](int, float (&v)[VEC]) {
+      block_range(hi, lo);
+      auto above = [&](float x) {
+        u64 c = 0;
+        again([&](int, float (&v)[VEC]) {
 #pragma unroll
           for (int e = 0; e < VEC; ++e)
-            if (v[e] > x && bucket(v[e]) == B) { ++c; w += weight(v[e]); }
+            if (v[e] > x && bucket(v[e]) == B) c += weighed ? weight(v[e]) : 1;
         });
-        block_sum(c, w, cn, cw);
-        cn += over; cw += over_mass;
+        return over + block_sum(c);
       };
       unsigned in = order_key(hi), out = order_key(lo) - 1;   // the end is the smallest key above which too little lies
-      u64 cn, cw;
       while (in - out > 1) {
         const unsigned mid = out + (in - out) / 2;
-        above(key_value(mid), cn, cw);
-        if (cn < need_n && cw < need_w) in = mid; else out = mid;
+        if (above(key_value(mid)) < need) in = mid; else out = mid;
       }
       const float x = key_value(in);
-      above(x, cn, cw);
-      u64 same = 0, d0;
-      all([&](int, float (&v)[VEC]) {
+      const u64 c = above(x);
+      u64 same = 0;
+      again([&](int, float (&v)[VEC]) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) same += v[e] == x;
       });
-      block_sum(same, 0, same, d0);
-      if (tid == 0) { end.value = x; end.over = (unsigned)cn; end.over_mass = cw; end.equal = (unsigned)same; end.w = weight(x); }
+      same = block_sum(same);
+      if (tid == 0) { end.value = x; end.over = c; end.equal = (unsigned)same; end.w = weighed ? weight(x) : 1; }
       __syncthreads();
     };
-    const u64 never = ~0ull;
     bool cut_k = false;
-    if (by_k && locate(k, never)) {   // (fewer tokens of any weight than k: all stay)
-      if (by_p) {   // (its weights are summed: what of them k leaves)
-        settle(k, never);
-        Z = end.over_mass + (k - end.over) * end.w;
-      } else {
-        settle(k, never);
+    if (by_k) {
+      clear();
+      all([&](int, float (&v)[VEC]) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (v[e] >= floor_k) atomicAdd(&mass[bucket(v[e])], 1ull);
+      });
+      __syncthreads();
+      cut_k = locate(k);   // (fewer tokens of any weight, or of the least that stays, than k: all stay)
+      if (cut_k) {
+        settle(k, false);
+        cut = end.value;
+        equal = k - end.over;
+        some = equal < end.equal;
       }
-      cut_k = true;
-      cut = end.value;
-      equal = k - end.over;
-      some = equal < end.equal;
     }
     if (by_p) {
-      const double reach = (double)p * (double)Z;
-      const u64 need = (u64)ceil(reach);
-      __syncthreads();
-      if (locate(never, need)) {
-        settle(never, need);
+      clear();
+      // of the tokens that top-k leaves; without it what weighs less than half of (1 - p) / V cannot reach the end and is only summed
+      const u64 light = cut_k ? 0 : (u64)(0.5 * (1.0 - (double)p) / V * kOne);
+      const u64 at_cut = cut_k ? equal * weight(cut) : 0;
+      u64 sum = tid == 0 ? at_cut : 0;
+      if (tid == 0 && cut_k) atomicAdd(&mass[bucket(cut)], at_cut);
+      all([&](int, float (&v)[VEC]) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (v[e] > cut) {
+            const u64 w = weight(v[e]);
+            sum += w;
+            if (w > light) atomicAdd(&mass[bucket(v[e])], w);
+          }
+      });
+      const u64 need = (u64)ceil((double)p * (double)block_sum(sum));
+      if (locate(need)) {
+        settle(need, true);
         const u64 w = end.w, ties = cut_k && end.value == cut ? equal : end.equal;
-        const u64 stay = min(ties, (need - end.over_mass + w - 1) / w);
+        equal = min(ties, (need - end.over + w - 1) / w);
         cut = end.value;
-        equal = stay;
-        some = stay < end.equal;
+        some = equal < end.equal;
       }
     }
   }
 
   // which of those equal to the cut
   int last = 0x7fffffff;
-  float unused;
   if (some) {
     u64 ties = 0;
     all([&](int, float (&v)[VEC]) {
@@ -369,9 +380,20 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
     if (lane == 0) red[0][wave] = ties;
     __syncthreads();
     u64 before = 0;
-    for (int i = 0; i < wave; ++i) before += red[0][i];
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) before += i < wave ? red[0][i] : 0;
     if (equal - 1 >= before && equal - 1 < before + ties) {
-      const int at = find(equal - 1 - before, [&](float x, int) { return (u64)(x == cut); }, unused);
+      float unused;
+      auto is = [&](float x, int) { return (u64)(x == cut); };
+      auto sum = [&](int r) {
+        float v[VEC];
+        values(load(r), v);
+        u64 t = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) t += v[e] == cut;
+        return t;
+      };
+      const int at = find(equal - 1 - before, sum, is, unused);
       if (lane == 0) end.index = at;
     }
     __syncthreads();
@@ -383,15 +405,19 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
   }
 
   // the draw
+  const float from = fmaxf(cut, floor_x);
   auto stays = [&](float x, int i) -> u64 {
-    if (!(x > cut || (x == cut && x > kNegInf && i <= last))) return 0;
+    if (!(x >= from) || x == kNegInf || (x == cut && i > last)) return 0;
     const u64 w = weight(x);
     return w >= least ? w : 0;
   };
-  u64 mine = 0;
+  u64 part[HOLD > 0 ? HOLD : 1] = {}, mine = 0;   // the lane's sums by rounds
   all([&](int r, float (&v)[VEC]) {
+    u64 t = 0;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) mine += stays(v[e], first + (r * 64 + lane) * VEC + e);
+    for (int e = 0; e < VEC; ++e) t += stays(v[e], first + (r * 64 + lane) * VEC + e);
+    if (HOLD > 0) part[HOLD > 0 ? r : 0] = t;
+    mine += t;
   });
   mine = sum_u64(mine);
   __syncthreads();
@@ -399,12 +425,21 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
   __syncthreads();
   u64 before = 0, Z = 0;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) { if (i < wave) before += red[0][i]; Z += red[0][i]; }
+  for (int i = 0; i < WAVES; ++i) { before += i < wave ? red[0][i] : 0; Z += red[0][i]; }
   const double at = (double)a.u[row] * (double)Z;
   const u64 target = at > 0.0 ? (at < (double)Z ? min((u64)at, Z - 1) : Z - 1) : 0;   // (u outside of [0, 1): the nearest end; NaN: the first)
   if (target < before || target >= before + mine) return;
   float x = 0.f;
-  const int token = find(target - before, stays, x);
+  auto sum = [&](int r) {
+    if constexpr (HOLD > 0) return part[r];
+    float v[VEC];
+    values(load(r), v);
+    u64 t = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) t += stays(v[e], first + (r * 64 + lane) * VEC + e);
+    return t;
+  };
+  const int token = find(target - before, sum, stays, x);
   if (lane == 0) {
     a.token[row] = token;
     if (a.logprob) a.logprob[row] = (float)(((double)x - (double)top) * inv_t - log((double)Z / kOne));
@@ -413,10 +448,10 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
 
 template <class E>
 static void sample_launch(hipStream_t st, const SampleArgs& a) {
-  // (a piece more than the row's where it is not aligned)
-  const int room = a.vocab + 16 / (int)sizeof(E) - 1;
-  if (room <= 512 * 16) hipLaunchKernelGGL((sample_kernel<E, 8, 16>), dim3(a.rows), dim3(512), 0, st, a);
-  else if (room <= 1024 * 32 + 16) hipLaunchKernelGGL((sample_kernel<E, 16, 32 + 16 / sizeof(E)>), dim3(a.rows), dim3(1024), 0, st, a);
+  // pieces of 16 bytes, one more than the row's where it is not aligned
+  const int pieces = (a.vocab * (int)sizeof(E) + 15) / 16 + 1;
+  if (pieces <= 512 * 4) hipLaunchKernelGGL((sample_kernel<E, 8, 4>), dim3(a.rows), dim3(512), 0, st, a);
+  else if (pieces <= 1024 * 9) hipLaunchKernelGGL((sample_kernel<E, 16, 9>), dim3(a.rows), dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((sample_kernel<E, 16, 0>), dim3(a.rows), dim3(1024), 0, st, a);
 }
 
