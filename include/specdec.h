@@ -410,7 +410,7 @@ int specdec_tree_visible(specdec_ctx* ctx, const int32_t* parent, int32_t B, int
  * u of their total; logprob (nullable) = the logarithm of its share of that total.  Temperature 0 (or less, or NaN): the largest logit,
  * lowest index first, logprob 0.  Logits of -inf and NaN are never drawn; +inf outweigh all else; a row without a logit above -inf has token -1
  * and logprob -inf.  Settings are fp32 (top_k: int32) [rows], null: temperature 1, the others off.
- * Sums are whole numbers, weights rounded to nearest multiples of 2^-38 of the largest: the same call gives the same tokens. */
+ * Sums are of whole numbers, weights to 2^-38 of the largest: the same call gives the same tokens. */
 int specdec_sample(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, int32_t rows, int32_t vocab, int64_t row_stride,
                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
                    int32_t* token, float* logprob, void* stream);

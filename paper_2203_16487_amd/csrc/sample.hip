@@ -5,7 +5,7 @@
 // first one always stays.  Every rule keeps a leading part of the same order, so what stays is a smallest logit, which of those
 // equal to it, and a smallest weight.  The token drawn is the first one, in the order of the vocabulary, at which the sum of the weights that
 // stay exceeds u of their total.
-// Weights are whole numbers, w 2^38 rounded to nearest from 64-bit floats, and their sums whole numbers of 64 bits: no order of
+// Weights are whole numbers, w 2^38 to less than one from 64-bit floats, and their sums whole numbers of 64 bits: no order of
 // summation changes a sum, so none changes a token.  (fp32 weights put the end of a nucleus one token off in about one row of a thousand:
 // sums are off by 1e-7, tokens at the end weigh 1e-4.)
 //
@@ -29,18 +29,25 @@ __device__ __forceinline__ unsigned order_key(float x) {
 }
 __device__ __forceinline__ float key_value(unsigned k) { return __builtin_bit_cast(float, k >> 31 ? k & 0x7fffffffu : ~k); }
 
-// round(2^38 2^t), t <= 0: whole and fractional part, the series of exp(f ln 2) to the power 10 (|f| <= 1/2: 2e-13 off)
-__device__ __forceinline__ u64 fixed_exp2(double t) {
-  if (t < -40.0) return 0;
-  constexpr double L = 0.69314718055994530942;
-  constexpr double c2 = L * L / 2, c3 = c2 * L / 3, c4 = c3 * L / 4, c5 = c4 * L / 5, c6 = c5 * L / 6, c7 = c6 * L / 7, c8 = c7 * L / 8, c9 = c8 * L / 9, c10 = c9 * L / 10;
-  const double n = __builtin_rint(t), f = t - n;
-  double p = c10;
-  p = __builtin_fma(p, f, c9); p = __builtin_fma(p, f, c8); p = __builtin_fma(p, f, c7); p = __builtin_fma(p, f, c6);
-  p = __builtin_fma(p, f, c5); p = __builtin_fma(p, f, c4); p = __builtin_fma(p, f, c3); p = __builtin_fma(p, f, c2);
-  p = __builtin_fma(p, f, L); p = __builtin_fma(p, f, 1.0);
-  const double r = __builtin_ldexp(p, (int)n + 38) + 4503599627370496.0;   // (2^52: what is behind the point is rounded away)
-  return __builtin_bit_cast(u64, r) & 0xfffffffffffffull;
+// 2^38 2^t, t = d * per <= 0, as a whole number (0 where d < least): 2^f for the fractional part |f| <= 1/2 by the polynomial that meets it
+// in nine Chebyshev nodes (relative error 2^-39.7), so off by less than one.  The whole part comes out of the low bits of t + 1.5 2^52, goes
+// into the exponent, and 2^52 added rounds what is behind the point away: fourteen 64-bit instructions.
+__device__ __forceinline__ u64 fixed_exp2(double d, double per, double least) {
+  constexpr double M = 6755399441055744.0;
+  const double m = __builtin_fma(d, per, M), f = __builtin_fma(d, per, -(m - M));
+  double p = 1.325497460306718e-06;
+  p = __builtin_fma(p, f, 1.531007807039615e-05);
+  p = __builtin_fma(p, f, 0.00015403457039410448);
+  p = __builtin_fma(p, f, 0.0013333450573018062);
+  p = __builtin_fma(p, f, 0.009618129157656703);
+  p = __builtin_fma(p, f, 0.055504109412010456);
+  p = __builtin_fma(p, f, 0.24022650695821055);
+  p = __builtin_fma(p, f, 0.6931471805459343);
+  p = __builtin_fma(p, f, 0.9999999999999997);
+  const u64 bits = __builtin_bit_cast(u64, p);
+  const unsigned hi = (unsigned)(bits >> 32) + (((unsigned)__builtin_bit_cast(u64, m) + 38u) << 20);
+  const u64 r = __builtin_bit_cast(u64, __builtin_bit_cast(double, (u64)hi << 32 | (unsigned)bits) + 4503599627370496.0) & 0xfffffffffffffull;
+  return d >= least ? r : 0;
 }
 
 // Sum over the wave, to every lane (the moves of wave_sum).
@@ -66,8 +73,9 @@ __device__ __forceinline__ u64 scan_u64(u64 v) {   // inclusive, over the lanes
 
 // HOLD 16-byte pieces a lane in registers; 0: read again for every pass.
 template <class E, int WAVES, int HOLD>
-__global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   constexpr int VEC = 16 / sizeof(E), THREADS = 64 * WAVES, EACH = kBuckets / THREADS;
+  constexpr int GROUP = HOLD > 9 ? 3 : 1, PARTS = HOLD > 0 ? (HOLD + GROUP - 1) / GROUP : 1;   // rounds whose sums a lane keeps as one
   typedef E Vec __attribute__((ext_vector_type(VEC)));
   typedef unsigned Raw __attribute__((ext_vector_type(4)));
   __shared__ u64 mass[kBuckets];      // (of counts, where the end of top-k is looked for)
@@ -164,7 +172,20 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) { top = fmaxf(top, v[e]); low = fminf(low, v[e] == kNegInf ? -kNegInf : v[e]); }
   });
+  // The smallest of the maxima of k or more groups of lanes: k tokens are at least as large, and few others, so only they are counted for top-k.
+  float among = kNegInf;
+  if (k > 0 && k <= THREADS) {
+    float m = top;
+    if (k <= THREADS / 4) { m = fmaxf(m, dpp_f<kDppSwap1>(m)); m = fmaxf(m, dpp_f<kDppSwap2>(m)); }
+    if (k <= THREADS / 16) { m = fmaxf(m, dpp_f<kDppHalfMirror>(m)); m = fmaxf(m, dpp_f<kDppMirror>(m)); }
+    among = -wave_max(-m);
+    if (lane == 0) red[1][wave] = __builtin_bit_cast(unsigned, among);
+  }
   block_range(top, low);
+  if (k > 0 && k <= THREADS) {
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) among = fminf(among, __builtin_bit_cast(float, (unsigned)red[1][i]));
+  }
   if (top == kNegInf) {   // nothing to draw from
     if (tid == 0) { a.token[row] = -1; if (a.logprob) a.logprob[row] = kNegInf; }
     return;
@@ -173,35 +194,44 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
 
   const bool alone = !(temperature > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;   // the first token is all that stays
   const double inv_t = 1.0 / (double)temperature, per_x = fmax(inv_t * 1.44269504088896340736, 1e-300);
-  auto weight = [&](float x) { return fixed_exp2(((double)x - (double)top) * per_x); };
+  const double weightless = -45.0 / per_x;
+  auto weight = [&](float x) { return fixed_exp2((double)x - (double)top, per_x, weightless); };
   const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * kOne) : 0;
   // below floor_0 nothing weighs anything, below floor_x not `least`, by margins far beyond the rounding of these lines
   auto floor_of = [&](float nats) { return top - 1.0001f * temperature * (nats + 1e-4f) - 1e-6f * fabsf(top); };
   const float floor_0 = floor_of(27.1f), floor_x = least > 0 ? floor_of(0.6931472f * (38.f - __builtin_amdgcn_logf((float)least))) : floor_0;
 
-  // the first token, in the order of the vocabulary, at which the wave's sum of mine(value, index) exceeds `target`, which all of it does; sum(r): the
-  // lane's part of round r.  Called by one wave.
-  auto find = [&](u64 target, auto sum, auto mine, float& value) {
-    u64 upto = 0, s = 0;
-    int r = 0;
-    auto one = [&](int q) {
-      const u64 t = sum(q), total = sum_u64(t);
-      if (target < total) { r = q; s = t; return true; }
-      target -= total;
-      return false;
+  // the first token, in the order of the vocabulary, at which the wave's sum of mine(value, index) exceeds `target`, which all of it does; part: the lane's
+  // sums by groups of rounds, where they are known.  Called by one wave.
+  auto find = [&](u64 target, const u64* part, auto mine, float& value) {
+    float v[VEC];
+    auto of_round = [&](int r) {
+      const int i0 = first + (r * 64 + lane) * VEC;
+      values(load(r), v);
+      u64 t = 0;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) t += mine(v[e], i0 + e);
+      return t;
     };
-    if constexpr (HOLD > 0) {
+    int r = 0;
+    if (HOLD > 0 && part) {
       bool got = false;
 #pragma unroll
-      for (int q = 0; q < HOLD; ++q)
-        if (q < rounds && !got) got = one(q);
-    } else {
-      while (!one(r)) ++r;
+      for (int q = 0; q < PARTS; ++q)
+        if (!got) {
+          const u64 total = sum_u64(part[q]);
+          if (target < total) { got = true; r = q * GROUP; } else target -= total;
+        }
     }
-    upto = scan_u64(s);
+    u64 s;
+    for (;; ++r) {
+      s = of_round(r);
+      const u64 total = sum_u64(s);
+      if (target < total) break;
+      target -= total;
+    }
+    const u64 upto = scan_u64(s);
     const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > target));
-    float v[VEC];
-    values(load(r), v);
     const int i0 = first + (r * 64 + lane) * VEC;
     u64 left = target - (upto - s);
     int at = -1;
@@ -224,7 +254,7 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
   if (by_k || by_p) {
     const float range = fminf(27.1f * temperature, (top - low) * 1.001f);   // (2^-39 = exp(-27.03))
     const float steps = (float)(kBuckets - 1) / range;
-    const float floor_k = by_p ? floor_0 : floor_x;   // (what min-p drops counts for top-p)
+    const float floor_k = fmaxf(by_p ? floor_0 : floor_x, by_k && !inf_top ? among : kNegInf);   // (what min-p drops counts for top-p)
     auto bucket = [&](float x) {
       const float d = top - x;
       return d > 0.f ? (int)fminf(d * steps, (float)(kBuckets - 1)) : 0;
@@ -384,16 +414,7 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
     for (int i = 0; i < WAVES; ++i) before += i < wave ? red[0][i] : 0;
     if (equal - 1 >= before && equal - 1 < before + ties) {
       float unused;
-      auto is = [&](float x, int) { return (u64)(x == cut); };
-      auto sum = [&](int r) {
-        float v[VEC];
-        values(load(r), v);
-        u64 t = 0;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) t += v[e] == cut;
-        return t;
-      };
-      const int at = find(equal - 1 - before, sum, is, unused);
+      const int at = find(equal - 1 - before, nullptr, [&](float x, int) { return (u64)(x == cut); }, unused);
       if (lane == 0) end.index = at;
     }
     __syncthreads();
@@ -411,12 +432,12 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
     const u64 w = weight(x);
     return w >= least ? w : 0;
   };
-  u64 part[HOLD > 0 ? HOLD : 1] = {}, mine = 0;   // the lane's sums by rounds
+  u64 part[PARTS] = {}, mine = 0;
   all([&](int r, float (&v)[VEC]) {
     u64 t = 0;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) t += stays(v[e], first + (r * 64 + lane) * VEC + e);
-    if (HOLD > 0) part[HOLD > 0 ? r : 0] = t;
+    if (HOLD > 0) part[HOLD > 0 ? r / GROUP : 0] += t;
     mine += t;
   });
   mine = sum_u64(mine);
@@ -430,16 +451,7 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
   const u64 target = at > 0.0 ? (at < (double)Z ? min((u64)at, Z - 1) : Z - 1) : 0;   // (u outside of [0, 1): the nearest end; NaN: the first)
   if (target < before || target >= before + mine) return;
   float x = 0.f;
-  auto sum = [&](int r) {
-    if constexpr (HOLD > 0) return part[r];
-    float v[VEC];
-    values(load(r), v);
-    u64 t = 0;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) t += stays(v[e], first + (r * 64 + lane) * VEC + e);
-    return t;
-  };
-  const int token = find(target - before, sum, stays, x);
+  const int token = find(target - before, HOLD > 0 ? part : nullptr, stays, x);
   if (lane == 0) {
     a.token[row] = token;
     if (a.logprob) a.logprob[row] = (float)(((double)x - (double)top) * inv_t - log((double)Z / kOne));
@@ -448,10 +460,13 @@ __global__ __launch_bounds__(64 * WAVES) void sample_kernel(SampleArgs a) {
 
 template <class E>
 static void sample_launch(hipStream_t st, const SampleArgs& a) {
-  // pieces of 16 bytes, one more than the row's where it is not aligned
+  // Pieces of 16 bytes, one more than the row's where it is not aligned.  A row of up to 144 KB stays in registers: with the rows for it two a compute
+  // unit, one loading while the other one computes; a few rows have more lanes each.
   const int pieces = (a.vocab * (int)sizeof(E) + 15) / 16 + 1;
   if (pieces <= 512 * 4) hipLaunchKernelGGL((sample_kernel<E, 8, 4>), dim3(a.rows), dim3(512), 0, st, a);
+  else if (pieces <= 512 * 18 && a.rows > 256) hipLaunchKernelGGL((sample_kernel<E, 8, 18>), dim3(a.rows), dim3(512), 0, st, a);
   else if (pieces <= 1024 * 9) hipLaunchKernelGGL((sample_kernel<E, 16, 9>), dim3(a.rows), dim3(1024), 0, st, a);
+  else if (pieces <= 1024 * 17) hipLaunchKernelGGL((sample_kernel<E, 16, 17>), dim3(a.rows), dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((sample_kernel<E, 16, 0>), dim3(a.rows), dim3(1024), 0, st, a);
 }
 
