@@ -104,20 +104,17 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     for (int r = 0; r < HOLD; ++r)
       if (r < rounds) held[r] = load(r);
   }
-  float top = kNegInf, low = -kNegInf;
+  float top = kNegInf;
   bool inf_top = false;   // only the infinite ones count: as zeros among -inf
   auto values = [&](Raw raw, float (&v)[VEC]) {
     const Vec p = __builtin_bit_cast(Vec, raw);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      v[e] = (float)p[e];
-      v[e] = v[e] == v[e] ? v[e] : kNegInf;
-    }
+    for (int e = 0; e < VEC; ++e) v[e] = (float)p[e];
     if (inf_top)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[e] = v[e] == -kNegInf ? 0.f : kNegInf;
   };
-  // f(round, the lane's values) for every round
+  // f(round, the lane's values) for every round.  NaN are among them: every use is a comparison that fails for them.
   auto all = [&](auto f) {
     float v[VEC];
     if constexpr (HOLD > 0) {
@@ -170,7 +167,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   const int k = a.top_k ? a.top_k[row] : 0;
   all([&](int, float (&v)[VEC]) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) { top = fmaxf(top, v[e]); low = fminf(low, v[e] == kNegInf ? -kNegInf : v[e]); }
+    for (int e = 0; e < VEC; ++e) top = v[e] > top ? v[e] : top;
   });
   // The smallest of the maxima of k or more groups of lanes: k tokens are at least as large, and few others, so only they are counted for top-k.
   float among = kNegInf;
@@ -181,7 +178,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     among = -wave_max(-m);
     if (lane == 0) red[1][wave] = __builtin_bit_cast(unsigned, among);
   }
-  block_range(top, low);
+  float unused = 0.f;
+  block_range(top, unused);
   if (k > 0 && k <= THREADS) {
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) among = fminf(among, __builtin_bit_cast(float, (unsigned)red[1][i]));
@@ -190,7 +188,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     if (tid == 0) { a.token[row] = -1; if (a.logprob) a.logprob[row] = kNegInf; }
     return;
   }
-  if (top == -kNegInf) { inf_top = true; top = low = 0.f; }
+  if (top == -kNegInf) { inf_top = true; top = 0.f; }
 
   const bool alone = !(temperature > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;   // the first token is all that stays
   const double inv_t = 1.0 / (double)temperature, per_x = fmax(inv_t * 1.44269504088896340736, 1e-300);
@@ -223,13 +221,14 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
           if (target < total) { got = true; r = q * GROUP; } else target -= total;
         }
     }
-    u64 s;
-    for (;; ++r) {
+    u64 s = 0;
+    for (; r < rounds; ++r) {
       s = of_round(r);
       const u64 total = sum_u64(s);
       if (target < total) break;
       target -= total;
     }
+    if (r >= rounds) return -1;   // (only if the logits change meanwhile)
     const u64 upto = scan_u64(s);
     const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > target));
     const int i0 = first + (r * 64 + lane) * VEC;
@@ -252,13 +251,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   bool some = alone;   // not all of those equal to it
   const bool by_k = !alone && k > 0 && k < V, by_p = !alone && p < 1.f;
   if (by_k || by_p) {
-    const float range = fminf(27.1f * temperature, (top - low) * 1.001f);   // (2^-39 = exp(-27.03))
-    const float steps = (float)(kBuckets - 1) / range;
+    const float steps = fminf((float)(kBuckets - 1) / (27.1f * temperature), 1e38f);   // (2^-39 = exp(-27.03): what is beyond weighs nothing)
     const float floor_k = fmaxf(by_p ? floor_0 : floor_x, by_k && !inf_top ? among : kNegInf);   // (what min-p drops counts for top-p)
-    auto bucket = [&](float x) {
-      const float d = top - x;
-      return d > 0.f ? (int)fminf(d * steps, (float)(kBuckets - 1)) : 0;
-    };
+    auto bucket = [&](float x) { return (int)fminf((top - x) * steps, (float)(kBuckets - 1)); };
     auto clear = [&] {
       __syncthreads();
       for (int i = tid; i < kBuckets; i += THREADS) mass[i] = 0;
@@ -292,10 +287,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     auto settle = [&](u64 need, bool weighed) {
       const int B = end.bucket;
       const u64 over = end.over;
+      // (every value of the step, and few others: by more than the rounding of a bucket)
+      const float wide = 1e-6f * fabsf(top), from = fmaxf(floor_k, top - ((float)B + 1.01f) / steps - wide), to = top - ((float)B - 0.01f) / steps + wide;
       all([&](int, float (&v)[VEC]) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (v[e] >= floor_k && bucket(v[e]) == B) {
+          if (v[e] >= from && v[e] <= to && bucket(v[e]) == B) {
             const unsigned at = atomicAdd(&list_n, 1u);
             if (at < kList) list[at] = v[e];
           }
