@@ -29,10 +29,10 @@ __device__ __forceinline__ unsigned order_key(float x) {
 }
 __device__ __forceinline__ float key_value(unsigned k) { return __builtin_bit_cast(float, k >> 31 ? k & 0x7fffffffu : ~k); }
 
-// 2^38 2^t, t = d * per <= 0, as a whole number (0 where d < least): 2^f for the fractional part |f| <= 1/2 by the polynomial that meets it
+// 2^38 2^t, 0 >= t = d * per >= -46, as a whole number: 2^f for the fractional part |f| <= 1/2 by the polynomial that meets it
 // in nine Chebyshev nodes (relative error 2^-39.7), so off by less than one.  The whole part comes out of the low bits of t + 1.5 2^52, goes
-// into the exponent, and 2^52 added rounds what is behind the point away: fourteen 64-bit instructions.
-__device__ __forceinline__ u64 fixed_exp2(double d, double per, double least) {
+// into the exponent, and 2^52 added rounds what is behind the point away: fifteen 64-bit instructions with what comes before, 8 cycles each.
+__device__ __forceinline__ u64 fixed_exp2(double d, double per) {
   constexpr double M = 6755399441055744.0;
   const double m = __builtin_fma(d, per, M), f = __builtin_fma(d, per, -(m - M));
   double p = 1.325497460306718e-06;
@@ -46,8 +46,7 @@ __device__ __forceinline__ u64 fixed_exp2(double d, double per, double least) {
   p = __builtin_fma(p, f, 0.9999999999999997);
   const u64 bits = __builtin_bit_cast(u64, p);
   const unsigned hi = (unsigned)(bits >> 32) + (((unsigned)__builtin_bit_cast(u64, m) + 38u) << 20);
-  const u64 r = __builtin_bit_cast(u64, __builtin_bit_cast(double, (u64)hi << 32 | (unsigned)bits) + 4503599627370496.0) & 0xfffffffffffffull;
-  return d >= least ? r : 0;
+  return __builtin_bit_cast(u64, __builtin_bit_cast(double, (u64)hi << 32 | (unsigned)bits) + 4503599627370496.0) & 0xfffffffffffffull;
 }
 
 // Sum over the wave, to every lane (the moves of wave_sum).
@@ -65,10 +64,31 @@ __device__ __forceinline__ u64 sum_u64(u64 v) {
   v += dpp_u64<kDppMirror>(v);
   return lane_u64(v, 0) + lane_u64(v, 16) + lane_u64(v, 32) + lane_u64(v, 48);
 }
-__device__ __forceinline__ u64 scan_u64(u64 v) {   // inclusive, over the lanes
-  const int lane = threadIdx.x & 63;
-  for (int o = 1; o < 64; o <<= 1) { const u64 x = __shfl_up(v, o); if (lane >= o) v += x; }
-  return v;
+// Inclusive running sum over the lanes: within rows of 16 by shifts, then the last lane of a row into the rows behind it.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp_add_u64(u64 v) {
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+  const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  return v + ((u64)hi << 32 | lo);
+}
+__device__ __forceinline__ u64 scan_u64(u64 v) {
+  v = dpp_add_u64<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8
+  v = dpp_add_u64<0x112, 0xf>(v);
+  v = dpp_add_u64<0x114, 0xf>(v);
+  v = dpp_add_u64<0x118, 0xf>(v);
+  v = dpp_add_u64<0x142, 0xa>(v);   // lane 15 of rows 0, 2 into 1, 3
+  return dpp_add_u64<0x143, 0xc>(v);   // lane 31 into rows 2, 3
+}
+
+// The values of four bytes.  (As instructions that are not merged with those of another pass.)
+__device__ __forceinline__ void unpack(unsigned raw, float* v, float) { v[0] = __builtin_bit_cast(float, raw); }
+__device__ __forceinline__ void unpack(unsigned raw, float* v, bf16) {
+  asm volatile("v_lshlrev_b32 %0, 16, %1" : "=v"(v[0]) : "v"(raw));
+  asm volatile("v_and_b32 %0, 0xffff0000, %1" : "=v"(v[1]) : "v"(raw));
+}
+__device__ __forceinline__ void unpack(unsigned raw, float* v, f16) {
+  asm volatile("v_cvt_f32_f16 %0, %1" : "=v"(v[0]) : "v"(raw));
+  asm volatile("v_cvt_f32_f16_sdwa %0, %1 src0_sel:WORD_1" : "=v"(v[1]) : "v"(raw));
 }
 
 // HOLD 16-byte pieces a lane in registers; 0: read again for every pass.
@@ -81,7 +101,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   __shared__ u64 mass[kBuckets];      // (of counts, where the end of top-k is looked for)
   __shared__ float list[kList];
   __shared__ u64 list_w[kList];
-  __shared__ u64 red[2][WAVES];
+  __shared__ u64 red[4][WAVES];         // (a place for each use: none waits until another one has been read)
+  __shared__ float red_f[2][WAVES];
   __shared__ unsigned list_n;
   __shared__ struct { u64 over, w; float value; unsigned equal; int bucket, index; } end;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x, V = a.vocab;
@@ -104,12 +125,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     for (int r = 0; r < HOLD; ++r)
       if (r < rounds) held[r] = load(r);
   }
+  for (int i = tid; i < kBuckets; i += THREADS) mass[i] = 0;
   float top = kNegInf;
   bool inf_top = false;   // only the infinite ones count: as zeros among -inf
   auto values = [&](Raw raw, float (&v)[VEC]) {
-    const Vec p = __builtin_bit_cast(Vec, raw);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) v[e] = (float)p[e];
+    for (int i = 0; i < 4; ++i) unpack(raw[i], v + i * (VEC / 4), E());
     if (inf_top)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[e] = v[e] == -kNegInf ? 0.f : kNegInf;
@@ -120,7 +141,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     if constexpr (HOLD > 0) {
 #pragma unroll
       for (int r = 0; r < HOLD; ++r) {
-        asm volatile("" : "+v"(held[r]));   // (nothing formed of the values outlives its pass, and rounds are not mixed: it would not fit the registers)
+        // (rounds are not mixed, and conversions do not outlive their pass: it would not fit the registers)
         if (r < rounds) { values(held[r], v); f(r, v); }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -142,7 +163,6 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   };
   auto block_sum = [&](u64 v) {   // to everyone
     v = sum_u64(v);
-    __syncthreads();
     if (lane == 0) red[0][wave] = v;
     __syncthreads();
     u64 s = 0;
@@ -153,14 +173,16 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   auto block_range = [&](float& hi, float& lo) {
     hi = wave_max(hi);
     lo = -wave_max(-lo);
-    __syncthreads();
-    if (lane == 0) red[0][wave] = (u64)__builtin_bit_cast(unsigned, hi) << 32 | __builtin_bit_cast(unsigned, lo);
+    if (lane == 0) { red_f[0][wave] = hi; red_f[1][wave] = lo; }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-      hi = fmaxf(hi, __builtin_bit_cast(float, (unsigned)(red[0][i] >> 32)));
-      lo = fminf(lo, __builtin_bit_cast(float, (unsigned)red[0][i]));
-    }
+    for (int i = 0; i < WAVES; ++i) { hi = fmaxf(hi, red_f[0][i]); lo = fminf(lo, red_f[1][i]); }
+  };
+  auto any = [](const float (&v)[VEC], auto is) {   // (one branch a piece)
+    bool r = false;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) r |= is(v[e]);
+    return r;
   };
 
   const float temperature = a.temperature ? a.temperature[row] : 1.f, p = a.top_p ? a.top_p[row] : 1.f, min_p = a.min_p ? a.min_p[row] : 0.f;
@@ -170,20 +192,15 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     for (int e = 0; e < VEC; ++e) top = v[e] > top ? v[e] : top;
   });
   // The smallest of the maxima of k or more groups of lanes: k tokens are at least as large, and few others, so only they are counted for top-k.
-  float among = kNegInf;
+  float among = -kNegInf;
   if (k > 0 && k <= THREADS) {
     float m = top;
     if (k <= THREADS / 4) { m = fmaxf(m, dpp_f<kDppSwap1>(m)); m = fmaxf(m, dpp_f<kDppSwap2>(m)); }
     if (k <= THREADS / 16) { m = fmaxf(m, dpp_f<kDppHalfMirror>(m)); m = fmaxf(m, dpp_f<kDppMirror>(m)); }
-    among = -wave_max(-m);
-    if (lane == 0) red[1][wave] = __builtin_bit_cast(unsigned, among);
+    among = m;
   }
-  float unused = 0.f;
-  block_range(top, unused);
-  if (k > 0 && k <= THREADS) {
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) among = fminf(among, __builtin_bit_cast(float, (unsigned)red[1][i]));
-  }
+  block_range(top, among);
+  if (among == -kNegInf) among = kNegInf;
   if (top == kNegInf) {   // nothing to draw from
     if (tid == 0) { a.token[row] = -1; if (a.logprob) a.logprob[row] = kNegInf; }
     return;
@@ -192,12 +209,17 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
 
   const bool alone = !(temperature > 0.f) || k == 1 || p <= 0.f || min_p > 1.f;   // the first token is all that stays
   const double inv_t = 1.0 / (double)temperature, per_x = fmax(inv_t * 1.44269504088896340736, 1e-300);
-  const double weightless = -45.0 / per_x;
-  auto weight = [&](float x) { return fixed_exp2((double)x - (double)top, per_x, weightless); };
   const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * kOne) : 0;
   // below floor_0 nothing weighs anything, below floor_x not `least`, by margins far beyond the rounding of these lines
-  auto floor_of = [&](float nats) { return top - 1.0001f * temperature * (nats + 1e-4f) - 1e-6f * fabsf(top); };
-  const float floor_0 = floor_of(27.1f), floor_x = least > 0 ? floor_of(0.6931472f * (38.f - __builtin_amdgcn_logf((float)least))) : floor_0;
+  auto floor_of = [&](float nats) { return fmaxf(top - 1.0001f * temperature * (nats + 1e-4f) - 1e-6f * fabsf(top), -3.402823466e38f); };
+  auto nats_of = [](float w) { return 0.6931472f * (38.f - __builtin_amdgcn_logf(w)); };   // from the largest down to a weight
+  const float floor_0 = floor_of(27.1f), floor_x = least > 0 ? floor_of(nats_of((float)least)) : floor_0;
+  const double weightless = -46.0 / per_x;
+  auto weight = [&](float x) {   // (four waves of a SIMD hide the chain's latency; several chains at once would not fit the registers)
+    const u64 w = fixed_exp2(fmax((double)x - (double)top, weightless), per_x);
+    __builtin_amdgcn_sched_barrier(0);
+    return w;
+  };
 
   // the first token, in the order of the vocabulary, at which the wave's sum of mine(value, index) exceeds `target`, which all of it does; part: the lane's
   // sums by groups of rounds, where they are known.  Called by one wave.
@@ -254,31 +276,22 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     const float steps = fminf((float)(kBuckets - 1) / (27.1f * temperature), 1e38f);   // (2^-39 = exp(-27.03): what is beyond weighs nothing)
     const float floor_k = fmaxf(by_p ? floor_0 : floor_x, by_k && !inf_top ? among : kNegInf);   // (what min-p drops counts for top-p)
     auto bucket = [&](float x) { return (int)fminf((top - x) * steps, (float)(kBuckets - 1)); };
-    auto clear = [&] {
-      __syncthreads();
-      for (int i = tid; i < kBuckets; i += THREADS) mass[i] = 0;
-      __syncthreads();
-    };
-    // the step in which the running sum reaches `need`; false: none does
+    // the step in which the running sum reaches `need`, behind a barrier; false: none does
     auto locate = [&](u64 need) {
-      u64 n = 0;
+      u64 n[EACH], sum = 0;
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) n += mass[tid * EACH + i];
-      const u64 un = scan_u64(n);
-      __syncthreads();
-      if (lane == 63) red[0][wave] = un;
+      for (int i = 0; i < EACH; ++i) { n[i] = mass[tid * EACH + i]; sum += n[i]; }
+      const u64 upto = scan_u64(sum);
+      if (lane == 63) red[1][wave] = upto;
       if (tid == 0) { end.bucket = -1; list_n = 0; }
       __syncthreads();
-      u64 bn = un - n;
+      u64 before = upto - sum;
 #pragma unroll
-      for (int i = 0; i < WAVES; ++i) bn += i < wave ? red[0][i] : 0;
-      if (bn < need && bn + n >= need) {
-#pragma unroll 1
-        for (int i = 0; i < EACH; ++i) {
-          const u64 cn = mass[tid * EACH + i];
-          if (bn + cn >= need) { end.bucket = tid * EACH + i; end.over = bn; break; }
-          bn += cn;
-        }
+      for (int i = 0; i < WAVES; ++i) before += i < wave ? red[1][i] : 0;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        if (before < need && before + n[i] >= need) { end.bucket = tid * EACH + i; end.over = before; }
+        before += n[i];
       }
       __syncthreads();
       return end.bucket >= 0;
@@ -290,6 +303,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       // (every value of the step, and few others: by more than the rounding of a bucket)
       const float wide = 1e-6f * fabsf(top), from = fmaxf(floor_k, top - ((float)B + 1.01f) / steps - wide), to = top - ((float)B - 0.01f) / steps + wide;
       all([&](int, float (&v)[VEC]) {
+        if (!any(v, [&](float x) { return x >= from && x <= to; })) return;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (v[e] >= from && v[e] <= to && bucket(v[e]) == B) {
@@ -332,6 +346,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
           for (int e = 0; e < VEC; ++e)
             if (v[e] > x && bucket(v[e]) == B) c += weighed ? weight(v[e]) : 1;
         });
+        __syncthreads();
         return over + block_sum(c);
       };
       unsigned in = order_key(hi), out = order_key(lo) - 1;   // the end is the smallest key above which too little lies
@@ -346,14 +361,15 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) same += v[e] == x;
       });
+      __syncthreads();
       same = block_sum(same);
       if (tid == 0) { end.value = x; end.over = c; end.equal = (unsigned)same; end.w = weighed ? weight(x) : 1; }
       __syncthreads();
     };
     bool cut_k = false;
     if (by_k) {
-      clear();
       all([&](int, float (&v)[VEC]) {
+        if (!any(v, [&](float x) { return x >= floor_k; })) return;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (v[e] >= floor_k) atomicAdd(&mass[bucket(v[e])], 1ull);
@@ -368,21 +384,37 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       }
     }
     if (by_p) {
-      clear();
-      // of the tokens that top-k leaves; without it what weighs less than half of (1 - p) / V cannot reach the end and is only summed
-      const u64 light = cut_k ? 0 : (u64)(0.5 * (1.0 - (double)p) / V * kOne);
-      const u64 at_cut = cut_k ? equal * weight(cut) : 0;
-      u64 sum = tid == 0 ? at_cut : 0;
-      if (tid == 0 && cut_k) atomicAdd(&mass[bucket(cut)], at_cut);
-      all([&](int, float (&v)[VEC]) {
+      if (by_k) {
+        for (int i = tid; i < kBuckets; i += THREADS) mass[i] = 0;   // (behind the barriers of locate and settle)
+        __syncthreads();
+      }
+      u64 sum = 0;
+      if (cut_k) {   // of the tokens that top-k leaves
+        if (tid == 0) {
+          sum = equal * weight(cut);
+          atomicAdd(&mass[bucket(cut)], sum);
+        }
+        all([&](int, float (&v)[VEC]) {
+          if (!any(v, [&](float x) { return x > cut; })) return;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (v[e] > cut) {
+          for (int e = 0; e < VEC; ++e)
+            if (v[e] > cut) {
+              const u64 w = weight(v[e]);
+              sum += w;
+              atomicAdd(&mass[bucket(v[e])], w);
+            }
+        });
+      } else {       // of all: what weighs less than half of (1 - p) / V cannot reach the end and is only summed
+        const float light = floor_of(nats_of(fmaxf(0.49f * (1.f - p) / (float)V * (float)kOne, 1.f)));
+        all([&](int, float (&v)[VEC]) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
             const u64 w = weight(v[e]);
             sum += w;
-            if (w > light) atomicAdd(&mass[bucket(v[e])], w);
+            if (v[e] >= light) atomicAdd(&mass[bucket(v[e])], w);
           }
-      });
+        });
+      }
       const u64 need = (u64)ceil((double)p * (double)block_sum(sum));
       if (locate(need)) {
         settle(need, true);
@@ -397,18 +429,17 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   // which of those equal to the cut
   int last = 0x7fffffff;
   if (some) {
-    u64 ties = 0;
+    unsigned count = 0;
     all([&](int, float (&v)[VEC]) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) ties += v[e] == cut;
+      for (int e = 0; e < VEC; ++e) count += v[e] == cut;
     });
-    ties = sum_u64(ties);
-    __syncthreads();
-    if (lane == 0) red[0][wave] = ties;
+    const u64 ties = sum_u64(count);
+    if (lane == 0) red[2][wave] = ties;
     __syncthreads();
     u64 before = 0;
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) before += i < wave ? red[0][i] : 0;
+    for (int i = 0; i < WAVES; ++i) before += i < wave ? red[2][i] : 0;
     if (equal - 1 >= before && equal - 1 < before + ties) {
       float unused;
       const int at = find(equal - 1 - before, nullptr, [&](float x, int) { return (u64)(x == cut); }, unused);
@@ -423,27 +454,32 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   }
 
   // the draw
-  const float from = fmaxf(cut, floor_x);
+  const float from = fmaxf(cut, floor_x);   // (finite: what is -inf or NaN is not above it)
   auto stays = [&](float x, int i) -> u64 {
-    if (!(x >= from) || x == kNegInf || (x == cut && i > last)) return 0;
+    if (!(x >= from) || (x == cut && i > last)) return 0;
     const u64 w = weight(x);
     return w >= least ? w : 0;
   };
   u64 part[PARTS] = {}, mine = 0;
+  const bool few = cut > kNegInf || least > 0;
   all([&](int r, float (&v)[VEC]) {
     u64 t = 0;
+    if (!few) {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) t += stays(v[e], first + (r * 64 + lane) * VEC + e);
+      for (int e = 0; e < VEC; ++e) t += weight(v[e]);
+    } else if (any(v, [&](float x) { return x >= from; })) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) t += stays(v[e], first + (r * 64 + lane) * VEC + e);
+    }
     if (HOLD > 0) part[HOLD > 0 ? r / GROUP : 0] += t;
     mine += t;
   });
   mine = sum_u64(mine);
-  __syncthreads();
-  if (lane == 0) red[0][wave] = mine;
+  if (lane == 0) red[3][wave] = mine;
   __syncthreads();
   u64 before = 0, Z = 0;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) { before += i < wave ? red[0][i] : 0; Z += red[0][i]; }
+  for (int i = 0; i < WAVES; ++i) { before += i < wave ? red[3][i] : 0; Z += red[3][i]; }
   const double at = (double)a.u[row] * (double)Z;
   const u64 target = at > 0.0 ? (at < (double)Z ? min((u64)at, Z - 1) : Z - 1) : 0;   // (u outside of [0, 1): the nearest end; NaN: the first)
   if (target < before || target >= before + mine) return;
