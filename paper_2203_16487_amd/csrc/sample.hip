@@ -146,13 +146,18 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      Raw next = load(0);
-      for (int r = 0; r < rounds; ++r) {
-        const Raw now = next;
-        if (r + 1 < rounds) next = load(r + 1);
-        values(now, v);
-        f(r, v);
-      }
+      constexpr int AHEAD = 4;
+      Raw next[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) next[i] = load(min(i, rounds - 1));
+#pragma unroll 1
+      for (int r = 0; r < rounds; r += AHEAD)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          const Raw now = next[i];
+          next[i] = load(min(r + i + AHEAD, rounds - 1));
+          if (r + i < rounds) { values(now, v); f(r + i, v); }
+        }
     }
   };
   // the same in few instructions, where it is seldom done
@@ -499,7 +504,6 @@ static void sample_launch(hipStream_t st, const SampleArgs& a) {
   if (pieces <= 512 * 4) hipLaunchKernelGGL((sample_kernel<E, 8, 4>), dim3(a.rows), dim3(512), 0, st, a);
   else if (pieces <= 512 * 18 && a.rows > 256) hipLaunchKernelGGL((sample_kernel<E, 8, 18>), dim3(a.rows), dim3(512), 0, st, a);
   else if (pieces <= 1024 * 9) hipLaunchKernelGGL((sample_kernel<E, 16, 9>), dim3(a.rows), dim3(1024), 0, st, a);
-  else if (pieces <= 1024 * 17) hipLaunchKernelGGL((sample_kernel<E, 16, 17>), dim3(a.rows), dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((sample_kernel<E, 16, 0>), dim3(a.rows), dim3(1024), 0, st, a);
 }
 
