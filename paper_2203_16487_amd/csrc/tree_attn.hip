@@ -47,15 +47,20 @@ struct TreePlan {
   int rw, kw, kt, row_blocks, target, slots;
   bool split;
 };
-constexpr int kSplitTarget = 512;
+#ifndef SPLIT_TARGET
+#define SPLIT_TARGET 512
+#endif
+constexpr int kSplitTarget = SPLIT_TARGET;
+// The workspace of a split call: tiles of a chunk, the first slot of every sequence (written by the first workgroup for tree_join_kernel); the slots.
+__host__ __device__ static constexpr size_t tree_head_ints(int B) { return ((size_t)B + 1 + 63) / 64 * 64; }
 static TreePlan tree_plan(const TreeAttnArgs& a) {
   TreePlan p;
   const int m = a.H / a.Hkv * a.T;
   p.rw = m <= 32 ? 1 : m <= 64 ? 2 : 4;
-  p.kw = 4 / p.rw;
-  p.kt = p.rw == 1 ? 128 : 64;
+  p.split = a.cap > 1024;
+  p.kw = p.rw == 4 ? 1 : p.rw == 2 || (p.split && a.dh == 128) ? 2 : 4;
+  p.kt = p.kw == 4 ? 128 : 64;
   p.row_blocks = (m + 32 * p.rw - 1) / (32 * p.rw);
-  p.split = a.cap > 8 * p.kt;
   p.target = kSplitTarget;
   const long whole = (long)a.B * a.Hkv * p.row_blocks;
   p.slots = (int)(p.split ? p.target + whole : whole);
@@ -136,6 +141,14 @@ __device__ __forceinline__ TreeWork tree_work(const TreeAttnArgs& a, const TreeP
   const TreeSeq held = tree_seq(a, p, min(lane, a.B - 1));
   auto seq = [&](int b) { return a.B <= 64 ? held : tree_seq(a, p, min(b, a.B - 1)); };
   const TreeDeal d = tree_deal(a, p, seq);
+  if (blockIdx.x == 0 && threadIdx.x < 64) {
+    int* head = reinterpret_cast<int*>(a.ws);
+    if (lane == 0) head[0] = d.per;
+    tree_slots(a, d.per, seq, [&](int first, int, int b0, const TreeSeq&) {
+      if (b0 + lane < a.B) head[1 + b0 + lane] = first;
+      return false;
+    });
+  }
   // neighbours in slot order, which share keys where a key head has several column blocks, go to one XCD
   const int each = (d.all + 7) / 8, at = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
   w.none = (int)(blockIdx.x >> 3) >= each || at >= d.all;
@@ -149,9 +162,9 @@ __device__ __forceinline__ TreeWork tree_work(const TreeAttnArgs& a, const TreeP
     int rest = at - __shfl(first, from);
     w.per = d.per;
     w.chunks = (s.tiles + d.per - 1) / d.per;
-    w.hk = rest / (s.blocks * w.chunks); rest -= w.hk * s.blocks * w.chunks;
-    w.chunk = rest / s.blocks;
-    w.block = rest - w.chunk * s.blocks;
+    w.chunk = rest / (s.blocks * a.Hkv); rest -= w.chunk * s.blocks * a.Hkv;
+    w.hk = rest / s.blocks;
+    w.block = rest - w.hk * s.blocks;
     w.slot = at;
     return true;
   });
@@ -320,7 +333,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   sum = half_add(sum);
 
   const bool whole = w.chunks == 1;
-  float* slot = a.ws + (size_t)w.slot * 32 * RW * (DH + 2);   // [columns][DH], [columns] maxima, [columns] sums
+  float* slot = a.ws + tree_head_ints(a.B) + (size_t)w.slot * 32 * RW * (DH + 2);   // [columns][DH], [columns] maxima, [columns] sums
   if constexpr (KW == 1) {
     if (!there) return;
     if (whole) {
@@ -396,54 +409,79 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   }
 }
 
-// The chunks of a (row, query head) added up: a workgroup each, its waves taking every fourth chunk.
-constexpr int kJoinWaves = 4;
-template <class E, int PER>
-__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreeAttnArgs a, TreePlan p) {
-  constexpr int DH = 64 * PER;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = blockIdx.x % a.H, t = blockIdx.x / a.H, b = blockIdx.y;
+// The chunks of a column (row, query head) added up, kJoinAhead of them requested at once: bound by round trips.  JW waves a column, each every JW-th
+// chunk: one, four columns a workgroup, where a column has few chunks, sixteen where it has many (64 chunks of 32 columns: 26 us with four waves
+// that first looked for the largest maximum).
+constexpr int kJoinAhead = 4;
+template <class E, int PER, int JW>
+__global__ __launch_bounds__(JW == 1 ? 256 : 64 * JW) void tree_join_kernel(TreeAttnArgs a, TreePlan p) {
+  constexpr int DH = 64 * PER, COLS = JW == 1 ? 4 : 1;
+  typedef float Part __attribute__((ext_vector_type(PER)));
+  typedef E Out __attribute__((ext_vector_type(PER)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cols = 32 * p.rw, G = a.H / a.Hkv;
+  int id = blockIdx.x;
+  const int c = id % (cols / COLS) * COLS + (JW == 1 ? wave : 0); id /= cols / COLS;
+  const int block = id % p.row_blocks; id /= p.row_blocks;
+  const int hk = id % a.Hkv, b = id / a.Hkv;
+  const int* head = reinterpret_cast<const int*>(a.ws);
+  const int per = head[0], first = head[1 + b];
   const TreeSeq s = tree_seq(a, p, b);
-  if (t >= s.rows) return;
-  const TreeSeq held = tree_seq(a, p, min(lane, a.B - 1));
-  auto seq = [&](int i) { return a.B <= 64 ? held : tree_seq(a, p, min(i, a.B - 1)); };
-  const TreeDeal d = tree_deal(a, p, seq);
-  const int chunks = (s.tiles + d.per - 1) / d.per;
-  if (chunks == 1) return;   // (written by its workgroup)
-  int first = 0;
-  tree_slots(a, d.per, seq, [&](int at, int, int b0, const TreeSeq&) {
-    if (b < b0 || b >= b0 + 64) return false;
-    first = __shfl(at, b - b0);
-    return true;
-  });
-  const int G = a.H / a.Hkv, m = t * G + h % G, block = m / (32 * p.rw), c = m - block * 32 * p.rw;
-  const size_t cols = 32 * p.rw, step = cols * (DH + 2) * s.blocks;
-  const float* slot = a.ws + ((size_t)first + (size_t)(h / G) * s.blocks * chunks + block) * cols * (DH + 2);
-  float top = kNegInf;
-  for (int i = lane; i < chunks; i += 64) top = fmaxf(top, slot[i * step + cols * DH + c]);
-  top = wave_max(top);
-  float o[PER] = {}, l = 0.f;
-#pragma unroll 4
-  for (int i = wave; i < chunks; i += kJoinWaves) {
-    const float mi = slot[i * step + cols * DH + c], li = slot[i * step + cols * (DH + 1) + c];
-    const float f = mi == kNegInf && li == 0.f ? 0.f : __builtin_amdgcn_exp2f(mi - top);
+  const int m = block * cols + c, chunks = (s.tiles + per - 1) / per;
+  if (m >= G * s.rows || chunks == 1) return;   // (one chunk: written by its workgroup)
+  const size_t step = (size_t)cols * (DH + 2) * s.blocks * a.Hkv;
+  const float* slot = a.ws + tree_head_ints(a.B) + ((size_t)first + (size_t)hk * s.blocks + block) * cols * (DH + 2);
+  Part o = {};
+  float top = kNegInf, l = 0.f;
+  auto add = [&](float mi, float li, const Part& v, float next) {
+    const float f = mi == kNegInf && li == 0.f ? 0.f : __builtin_amdgcn_exp2f(mi - next);
     l += f * li;
+    o += f * v;
+  };
+  for (int i0 = JW == 1 ? 0 : wave; i0 < chunks; i0 += JW * kJoinAhead) {
+    Part v[kJoinAhead];
+    float mi[kJoinAhead], li[kJoinAhead], next = top;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] += f * slot[i * step + (size_t)c * DH + e * 64 + lane];
+    for (int j = 0; j < kJoinAhead; ++j) {
+      const float* from = slot + min(i0 + j * JW, chunks - 1) * step;
+      v[j] = *reinterpret_cast<const Part*>(from + (size_t)c * DH + lane * PER);
+      mi[j] = from[cols * DH + c];
+      li[j] = from[cols * (DH + 1) + c];
+    }
+#pragma unroll
+    for (int j = 0; j < kJoinAhead; ++j) next = fmaxf(next, mi[j]);
+    const float keep = top == kNegInf && l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - next);
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (int j = 0; j < kJoinAhead; ++j)
+      if (i0 + j * JW < chunks) add(mi[j], li[j], v[j], next);
+    top = next;
   }
-  __shared__ float part[kJoinWaves][DH + 1];
+  if constexpr (JW > 1) {
+    __shared__ float part[JW][DH + 2];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) part[wave][e * 64 + lane] = o[e];
-  if (lane == 0) part[wave][DH] = l;
-  __syncthreads();
-  if (threadIdx.x >= DH) return;
-  float x = 0.f, y = 0.f;
-  for (int i = 0; i < kJoinWaves; ++i) { x += part[i][threadIdx.x]; y += part[i][DH]; }
-  static_cast<E*>(a.o)[b * a.o_s[0] + t * a.o_s[1] + h * a.o_s[2] + threadIdx.x] = (E)(y == 0.f ? 0.f : x / y);
+    for (int e = 0; e < PER; ++e) part[wave][lane * PER + e] = o[e];
+    if (lane == 0) { part[wave][DH] = top; part[wave][DH + 1] = l; }
+    __syncthreads();
+    if (wave != 0) return;
+    float next = kNegInf;
+#pragma unroll
+    for (int j = 0; j < JW; ++j) next = fmaxf(next, part[j][DH]);
+    l = 0.f;
+    o = Part{};
+#pragma unroll
+    for (int j = 0; j < JW; ++j) add(part[j][DH], part[j][DH + 1], *reinterpret_cast<const Part*>(&part[j][lane * PER]), next);
+  }
+  const int t = m / G;
+  Out x;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) x[e] = (E)(l == 0.f ? 0.f : o[e] / l);
+  *reinterpret_cast<Out*>(static_cast<E*>(a.o) + b * a.o_s[0] + t * a.o_s[1] + (hk * G + m - t * G) * a.o_s[2] + lane * PER) = x;
 }
 
 size_t tree_attn_bytes(const TreeAttnArgs& a) {
   const TreePlan p = tree_plan(a);
-  return p.split ? (size_t)p.slots * 32 * p.rw * (a.dh + 2) * sizeof(float) : 0;
+  return p.split ? (tree_head_ints(a.B) + (size_t)p.slots * 32 * p.rw * (a.dh + 2)) * sizeof(float) : 0;
 }
 
 template <class E, int DH, int RW, int KW, int SUB>
@@ -462,14 +500,17 @@ static hipError_t tree_launch(hipStream_t st, const TreeAttnArgs& a, const TreeP
   hipLaunchKernelGGL(kernel, dim3((unsigned)(p.split ? (p.slots + 7) / 8 * 8 : p.slots)), dim3(64 * RW * KW), bytes, st, a, p);
   e = hipGetLastError();
   if (e != hipSuccess || !p.split) return e;
-  hipLaunchKernelGGL((tree_join_kernel<E, DH / 64>), dim3(a.T * a.H, a.B), dim3(64 * kJoinWaves), 0, st, a, p);
+  // (a column has about as many chunks as the target is larger than the number of column blocks)
+  const unsigned columns = (unsigned)a.B * a.Hkv * p.row_blocks * 32 * p.rw;
+  if (p.target <= 8 * a.B * a.Hkv * p.row_blocks) hipLaunchKernelGGL((tree_join_kernel<E, DH / 64, 1>), dim3(columns / 4), dim3(256), 0, st, a, p);
+  else hipLaunchKernelGGL((tree_join_kernel<E, DH / 64, 16>), dim3(columns), dim3(1024), 0, st, a, p);
   return hipGetLastError();
 }
 
 template <class E, int DH>
 static hipError_t tree_launch_rows(hipStream_t st, const TreeAttnArgs& a) {
   const TreePlan p = tree_plan(a);
-  return p.rw == 1 ? tree_launch<E, DH, 1, 4, 1>(st, a, p) : p.rw == 2 ? tree_launch<E, DH, 2, 2, 1>(st, a, p) : tree_launch<E, DH, 4, 1, 2>(st, a, p);
+  return p.rw == 1 ? p.kw == 2 ? tree_launch<E, DH, 1, 2, 1>(st, a, p) : tree_launch<E, DH, 1, 4, 1>(st, a, p) : p.rw == 2 ? tree_launch<E, DH, 2, 2, 1>(st, a, p) : tree_launch<E, DH, 4, 1, 2>(st, a, p);
 }
 
 hipError_t tree_attn(hipStream_t st, const TreeAttnArgs& a) {
