@@ -20,12 +20,13 @@ namespace sd {
 typedef unsigned long long u64;
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-// What differs between the element types.  kLift: weights are stored as 2^kLift exp2(s - max), so that fp16, whose values end at 2^-24,
-// keeps weights down to 2^-38 of the largest: without it 65536 keys of 2^-25 each would be lost.
+// What differs between the element types.  A column's reference (the running maximum of a softmax) follows its scores only when they exceed it by
+// kSlack powers of two: sums are rescaled seldom.  kLift: weights are stored as 2^kLift exp2(s - reference), so that fp16, whose values end
+// at 2^-24, keeps weights down to 2^-37 of the largest (without it 65536 keys of 2^-25 each would be lost) and none reaches 2^16.
 template <class E> struct AttnType;
 template <> struct AttnType<bf16> {
   typedef bf16 x8 __attribute__((ext_vector_type(8)));
-  static constexpr float kLift = 0.f;
+  static constexpr float kLift = 0.f, kSlack = 8.f;
   static constexpr unsigned kExp = 0x7f807f80u, kUnit = 0x00800080u;
   static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -33,7 +34,7 @@ template <> struct AttnType<bf16> {
 };
 template <> struct AttnType<f16> {
   typedef f16 x8 __attribute__((ext_vector_type(8)));
-  static constexpr float kLift = 14.f;
+  static constexpr float kLift = 13.f, kSlack = 2.f;
   static constexpr unsigned kExp = 0x7c007c00u, kUnit = 0x04000400u;
   static __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -61,8 +62,8 @@ static TreePlan tree_plan(const TreeAttnArgs& a) {
   p.kw = p.rw == 4 ? 1 : p.rw == 2 || (p.split && a.dh == 128) ? 2 : 4;
   p.kt = p.kw == 4 ? 128 : 64;
   p.row_blocks = (m + 32 * p.rw - 1) / (32 * p.rw);
-  p.target = kSplitTarget;
   const long whole = (long)a.B * a.Hkv * p.row_blocks;
+  p.target = whole <= kSplitTarget * 3 / 4 ? kSplitTarget : 2 * kSplitTarget;
   p.slots = (int)(p.split ? p.target + whole : whole);
   return p;
 }
@@ -82,9 +83,12 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeAttnArgs& a, const TreePla
 // Where a workgroup's work lies: chunk `chunk` of `chunks` of `per` tiles, in slot `slot`.
 struct TreeWork { int b, hk, block, chunk, chunks, per, slot; bool none; };
 
-__device__ __forceinline__ int wave_sum_i(int v) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+__device__ __forceinline__ int wave_sum_i(int v) {   // (the moves of wave_sum)
+  v += dpp_i<kDppSwap1>(v);
+  v += dpp_i<kDppSwap2>(v);
+  v += dpp_i<kDppHalfMirror>(v);
+  v += dpp_i<kDppMirror>(v);
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
 }
 
 // (every wave for itself: lane i has sequences i, i + 64, ..)
@@ -101,12 +105,20 @@ __device__ __forceinline__ TreeDeal tree_deal(const TreeAttnArgs& a, const TreeP
   }
   TreeDeal d;
   d.per = max(1, (int)fmin(ceil(total * a.Hkv / p.target), 1073741824.0));
-  int all = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const TreeSeq s = seq(b0 + lane);
-    all += wave_sum_i(b0 + lane < a.B ? a.Hkv * s.blocks * ((s.tiles + d.per - 1) / d.per) : 0);
+  // Last chunks are short ones, so there are more than that.  A workgroup more than run at once doubles the time of all: chunks that are longer, until they
+  // fit, or until no sequence is cut any more.
+  for (int turn = 0;; ++turn) {
+    int all = 0, most = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      const TreeSeq s = seq(b0 + lane);
+      const bool in = b0 + lane < a.B;
+      all += wave_sum_i(in ? a.Hkv * s.blocks * ((s.tiles + d.per - 1) / d.per) : 0);
+      most = max(most, wave_max_i(in && s.blocks ? s.tiles : 0));
+    }
+    d.all = all;
+    if (all <= p.target || p.target > kSplitTarget || d.per >= most || turn == 8) break;
+    d.per = max(d.per + 1, (int)fmin(ceil((double)d.per * all / p.target), (double)most));
   }
-  d.all = all;
   return d;
 }
 // Running sums of the workgroups of the sequences: f(first slot of the lane's sequence, its slots, sequence) for 64 of them at a time.
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   const char* kb = reinterpret_cast<const char*>(static_cast<const E*>(a.k) + w.b * a.k_s[0] + w.hk * a.k_s[2]);
   const char* vb = reinterpret_cast<const char*>(static_cast<const E*>(a.v) + w.b * a.v_s[0] + w.hk * a.v_s[2]);
   const long krow = a.k_s[1] * 2, vrow = a.v_s[1] * 2;
-  auto load_tile = [&](int tile, int buf) {
+  auto load_tile = [&](int tile, int buf) __attribute__((always_inline)) {
     char* dst = lds + buf * 2 * TILE + wave * 1024;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
@@ -218,10 +230,13 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
     const E* qp = static_cast<const E*>(a.q) + w.b * a.q_s[0] + (there ? t : 0) * a.q_s[1] + (there ? head : w.hk * G) * a.q_s[2] + half * 8;
 #pragma unroll
     for (int k = 0; k < DH / 16; ++k) q[k] = *reinterpret_cast<const s16x8*>(qp + k * 16);
+    if (a.scale < 0.f)   // (a negative scale as queries of the other sign: the largest product is the largest score)
+#pragma unroll
+      for (int k = 0; k < DH / 16; ++k) q[k] ^= (short)0x8000;
   }
   u64 seen = 0;
   if (there) seen = (a.visible ? a.visible[(size_t)w.b * a.T + t] : ~0ull >> (63 - t)) & (~0ull >> (64 - s.rows));
-  const float scale = a.scale * 1.44269504088896f;
+  const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-37f);   // (not 0: what is masked is -inf times this)
 
   f32x16 acc[ET];
 #pragma unroll
@@ -231,7 +246,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   const int kc = swz(kkey) ^ half, vc = ((lane >> 4 & 1) * 2 + (g >> 1 & 1)) ^ swz(vkey);
 
   // 32 keys of the tile in buffer buf, from key `first` of it, `key` of the sequence
-  auto step = [&](auto masked, const char* kt, const char* vt, int first, int key) {
+  auto step = [&](auto masked, const char* kt, const char* vt, int first, int key) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(masked)::value;
     f32x16 st = {};
 #pragma unroll
@@ -247,32 +262,40 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
     float x[16], big = kNegInf;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      x[i] = st[i] * scale;
+      x[i] = st[i];
       if (MASK && !(window >> (8 * (i >> 2) + (i & 3)) & 1)) x[i] = kNegInf;
       big = fmaxf(big, x[i]);
     }
-    big = fmaxf(top, half_max(big));
-    const float base = big == kNegInf ? 0.f : big - Ty::kLift;
-    const float keep = __builtin_amdgcn_exp2f(top == kNegInf ? kNegInf : top - big);
-    float part = 0.f;
+    big = half_max(big) * scale;
+    if (__builtin_amdgcn_ballot_w64(big > top + Ty::kSlack)) {
+      const float next = fmaxf(top, big), keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      sum *= keep;
+      // (in place: as an ordinary product it is formed for every tile, and all sums are moved)
+#pragma unroll
+      for (int e = 0; e < ET; ++e) mfma_settle(acc[e]);
+#pragma unroll
+      for (int e = 0; e < ET; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float v = acc[e][i];
+          asm volatile("v_mul_f32 %0, %0, %1" : "+v"(v) : "v"(keep));
+          acc[e][i] = v;
+        }
+    }
+    const float base = top == kNegInf ? 0.f : top - Ty::kLift;
     s16x8 pf[2];
     typename Ty::x8 pv[2];
+    float part = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      x[i] = __builtin_amdgcn_exp2f(x[i] - base);
+      x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -base));
       part += x[i];
       pv[i >> 3][i & 7] = (E)x[i];
     }
     pf[0] = __builtin_bit_cast(s16x8, pv[0]);
     pf[1] = __builtin_bit_cast(s16x8, pv[1]);
-    sum = sum * keep + part;
-    if (__builtin_amdgcn_ballot_w64(big != top)) {
-#pragma unroll
-      for (int e = 0; e < ET; ++e)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[e][i] *= keep;
-    }
-    top = big;
+    sum += part;
     if constexpr (MASK) {
       // Values that some columns see and others do not: 0 x infinity is not 0.  Where the tree's rows of this tile hold any, products one by one.
       if (a.T > 1 || a.visible) {
@@ -315,18 +338,25 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   };
 
   const bool idle = (w.block * RW + wr) * 32 >= M;   // (a wave without columns: it loads and waits with the others)
-  for (int buf = 0; tile < end; ++tile, buf ^= 1) {
+  auto tile_in = [&](auto buffer) __attribute__((always_inline)) {   // (which buffer is known to the compiler: addresses in LDS are a lane's own and a constant)
+    constexpr int BUF = decltype(buffer)::value;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();   // every wave's part of this tile is there, and every wave is done with the buffer loaded next
-    if (tile + 1 < end) load_tile(tile + 1, buf ^ 1);
-    if (idle) continue;
-    const char* kt = lds + buf * 2 * TILE;
+    if (tile + 1 < end) load_tile(tile + 1, BUF ^ 1);
+    if (!idle) {
+      const char* kt = lds + BUF * 2 * TILE;
 #pragma unroll
-    for (int u = 0; u < SUB; ++u) {
-      const int first = (wk * SUB + u) * 32, key = tile * KT + first;
-      if (key + 32 <= s.n) step(std::false_type{}, kt, kt + TILE, first, key);
-      else if (key < s.n + s.rows) step(std::true_type{}, kt, kt + TILE, first, key);
+      for (int u = 0; u < SUB; ++u) {
+        const int first = (wk * SUB + u) * 32, key = tile * KT + first;
+        if (key + 32 <= s.n) step(std::false_type{}, kt, kt + TILE, first, key);
+        else if (key < s.n + s.rows) step(std::true_type{}, kt, kt + TILE, first, key);
+      }
     }
+    ++tile;
+  };
+  while (tile < end) {
+    tile_in(std::integral_constant<int, 0>{});
+    if (tile < end) tile_in(std::integral_constant<int, 1>{});
   }
 #pragma unroll
   for (int e = 0; e < ET; ++e) mfma_settle(acc[e]);
