@@ -268,20 +268,16 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
     }
     big = half_max(big) * scale;
     if (__builtin_amdgcn_ballot_w64(big > top + Ty::kSlack)) {
-      const float next = fmaxf(top, big), keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - next);
+      const float next = fmaxf(top, big);
+      float keep = top == kNegInf ? 0.f : __builtin_amdgcn_exp2f(top - next);
       top = next;
       sum *= keep;
-      // (in place: as an ordinary product it is formed for every tile, and all sums are moved)
+      asm volatile("" : "+v"(keep));   // (known here only: the products are not formed ahead for every tile)
 #pragma unroll
-      for (int e = 0; e < ET; ++e) mfma_settle(acc[e]);
+      for (int e = 0; e < ET; ++e) acc[e] *= keep;
+    } else {   // (a value of its own on this side, too: else all sums are moved to other registers and back, for every tile)
 #pragma unroll
-      for (int e = 0; e < ET; ++e)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float v = acc[e][i];
-          asm volatile("v_mul_f32 %0, %0, %1" : "+v"(v) : "v"(keep));
-          acc[e][i] = v;
-        }
+      for (int e = 0; e < ET; ++e) asm volatile("" : "+v"(acc[e]));
     }
     const float base = top == kNegInf ? 0.f : top - Ty::kLift;
     s16x8 pf[2];
