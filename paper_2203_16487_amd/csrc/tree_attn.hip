@@ -211,11 +211,32 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   const char* kb = reinterpret_cast<const char*>(static_cast<const E*>(a.k) + w.b * a.k_s[0] + w.hk * a.k_s[2]);
   const char* vb = reinterpret_cast<const char*>(static_cast<const E*>(a.v) + w.b * a.v_s[0] + w.hk * a.v_s[2]);
   const long krow = a.k_s[1] * 2, vrow = a.v_s[1] * 2;
+  // (a lane's place in a tile: the same for every load of it but for the swizzle where a wave's loads are 8 keys apart; rows so far apart
+  // that it passes 32 bits take the products for every load, as does the last tile, whose keys end)
+  constexpr int APART = WAVES * RPI;
+  const bool near = (krow | vrow) < (1l << 26);
+  unsigned kofs[2], vofs[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const unsigned chunk = ((lane % CH) ^ swz(key0 + i * APART)) * 16;
+    kofs[i] = (unsigned)key0 * (unsigned)krow + chunk;
+    vofs[i] = (unsigned)key0 * (unsigned)vrow + chunk;
+  }
+  static_assert(APART % 16 == 0 || APART == 8, "swizzles of every other load are alike");
   auto load_tile = [&](int tile, int buf) __attribute__((always_inline)) {
     char* dst = lds + buf * 2 * TILE + wave * 1024;
+    if (near && tile * KT + KT - 1 <= last) {
 #pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const long row = tile * KT + i * APART;
+        __builtin_amdgcn_global_load_lds(SD_GLB_PTR(kb + row * krow + kofs[i & 1]), SD_LDS_PTR(dst + i * WAVES * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(SD_GLB_PTR(vb + row * vrow + vofs[i & 1]), SD_LDS_PTR(dst + TILE + i * WAVES * 1024), 16, 0, 0);
+      }
+      return;
+    }
+#pragma unroll 1
     for (int i = 0; i < LOADS; ++i) {
-      const int in = key0 + i * WAVES * RPI, key = min(tile * KT + in, last);
+      const int in = key0 + i * APART, key = min(tile * KT + in, last);
       const int chunk = ((lane % CH) ^ swz(in)) * 16;
       __builtin_amdgcn_global_load_lds(SD_GLB_PTR(kb + key * krow + chunk), SD_LDS_PTR(dst + i * WAVES * 1024), 16, 0, 0);
       __builtin_amdgcn_global_load_lds(SD_GLB_PTR(vb + key * vrow + chunk), SD_LDS_PTR(dst + TILE + i * WAVES * 1024), 16, 0, 0);
@@ -245,27 +266,33 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   const int g = lane & 15, kkey = col, vkey = 4 * half + g / 4;
   const int kc = swz(kkey) ^ half, vc = ((lane >> 4 & 1) * 2 + (g >> 1 & 1)) ^ swz(vkey);
 
-  // 32 keys of the tile in buffer buf, from key `first` of it, `key` of the sequence
-  auto step = [&](auto masked, const char* kt, const char* vt, int first, int key) __attribute__((always_inline)) {
+  // 32 N keys from key `first` of a tile, `key` of the sequence.  (N > 1: one product's chain of matrix instructions fills the other one's waits.)
+  auto step = [&](auto masked, auto parts, const char* kt, const char* vt, int first, int key) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(masked)::value;
-    f32x16 st = {};
+    constexpr int N = decltype(parts)::value;
+    static_assert(!MASK || N == 1, "");
+    f32x16 st[N] = {};
 #pragma unroll
-    for (int k = 0; k < DH / 16; ++k) {
-      const s16x8 kf = *reinterpret_cast<const s16x8*>(kt + (first + kkey) * ROW + ((kc ^ 2 * k) * 16));
-      st = Ty::mfma(kf, q[k], st);
-    }
+    for (int k = 0; k < DH / 16; ++k)
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const s16x8 kf = *reinterpret_cast<const s16x8*>(kt + (first + 32 * u + kkey) * ROW + ((kc ^ 2 * k) * 16));
+        st[u] = Ty::mfma(kf, q[k], st[u]);
+      }
     unsigned window = ~0u;   // which of keys 4 half .. + 31 this column sees
     if constexpr (MASK) {
       const int rel = key + 4 * half - s.n;
       window = rel >= 64 ? 0u : rel >= 0 ? (unsigned)(seen >> rel) : rel <= -32 ? ~0u : (unsigned)(seen << -rel) | ((1u << -rel) - 1);
     }
-    float x[16], big = kNegInf;
+    float x[N][16], big = kNegInf;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] = st[i];
-      if (MASK && !(window >> (8 * (i >> 2) + (i & 3)) & 1)) x[i] = kNegInf;
-      big = fmaxf(big, x[i]);
-    }
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[u][i] = st[u][i];
+        if (MASK && !(window >> (8 * (i >> 2) + (i & 3)) & 1)) x[u][i] = kNegInf;
+        big = fmaxf(big, x[u][i]);
+      }
     big = half_max(big) * scale;
     if (__builtin_amdgcn_ballot_w64(big > top + Ty::kSlack)) {
       const float next = fmaxf(top, big);
@@ -280,17 +307,20 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
       for (int e = 0; e < ET; ++e) asm volatile("" : "+v"(acc[e]));
     }
     const float base = top == kNegInf ? 0.f : top - Ty::kLift;
-    s16x8 pf[2];
-    typename Ty::x8 pv[2];
+    s16x8 pf[2 * N];
     float part = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -base));
-      part += x[i];
-      pv[i >> 3][i & 7] = (E)x[i];
+    for (int u = 0; u < N; ++u) {
+      typename Ty::x8 pv[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], scale, -base));
+        part += x[u][i];
+        pv[i >> 3][i & 7] = (E)x[u][i];
+      }
+      pf[2 * u] = __builtin_bit_cast(s16x8, pv[0]);
+      pf[2 * u + 1] = __builtin_bit_cast(s16x8, pv[1]);
     }
-    pf[0] = __builtin_bit_cast(s16x8, pv[0]);
-    pf[1] = __builtin_bit_cast(s16x8, pv[1]);
     sum += part;
     if constexpr (MASK) {
       // Values that some columns see and others do not: 0 x infinity is not 0.  Where the tree's rows of this tile hold any, products one by one.
@@ -302,12 +332,14 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
           for (unsigned u : {v4.x, v4.y, v4.z, v4.w}) odd |= ((u & Ty::kExp) + Ty::kUnit) & 0x80008000u;
         }
         if (__builtin_amdgcn_ballot_w64(odd != 0)) {
+#pragma unroll 1
+          for (int i = 0; i < 32; ++i) {   // (seldom run, so short: the lane's weights move past, two keys each)
+            const int reg = i >> 1, h2 = i & 1, row = first + 8 * (reg >> 2) + 4 * h2 + (reg & 3);
+            const float pi = (float)(E)__shfl(x[0][0], col + 32 * h2);
+            if (h2)
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const int reg = (i >> 3) * 4 + (i & 3), h2 = i >> 2 & 1, row = first + i;
-            const float pi = (float)(E)__shfl(x[reg], col + 32 * h2);
-            const bool sees = __shfl(window, col + 32 * h2) >> (8 * (reg >> 2) + (reg & 3)) & 1;
-            if (sees)
+              for (int r = 0; r < 15; ++r) x[0][r] = x[0][r + 1];
+            if (__shfl(window, col + 32 * h2) >> (8 * (reg >> 2) + (reg & 3)) & 1)
 #pragma unroll
               for (int e = 0; e < ET; ++e)
 #pragma unroll
@@ -321,7 +353,7 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
       }
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2 * N; ++k)
 #pragma unroll
       for (int e = 0; e < ET; ++e) {
         s16x4 v4[2];
@@ -341,11 +373,13 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
     if (tile + 1 < end) load_tile(tile + 1, BUF ^ 1);
     if (!idle) {
       const char* kt = lds + BUF * 2 * TILE;
-#pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        const int first = (wk * SUB + u) * 32, key = tile * KT + first;
-        if (key + 32 <= s.n) step(std::false_type{}, kt, kt + TILE, first, key);
-        else if (key < s.n + s.rows) step(std::true_type{}, kt, kt + TILE, first, key);
+      const int first = wk * SUB * 32, key = tile * KT + first;
+      if (key + 32 * SUB <= s.n) {
+        step(std::false_type{}, std::integral_constant<int, SUB>{}, kt, kt + TILE, first, key);
+      } else {
+#pragma unroll 1
+        for (int u = 0; u < 32 * SUB && key + u < s.n + s.rows; u += 32)
+          step(std::true_type{}, std::integral_constant<int, 1>{}, kt, kt + TILE, first + u, key + u);
       }
     }
     ++tile;
