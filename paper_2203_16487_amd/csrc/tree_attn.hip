@@ -366,27 +366,42 @@ __global__ __launch_bounds__(64 * RW * KW, 2) void tree_attn_kernel(TreeAttnArgs
   };
 
   const bool idle = (w.block * RW + wr) * 32 >= M;   // (a wave without columns: it loads and waits with the others)
-  auto tile_in = [&](auto buffer) __attribute__((always_inline)) {   // (which buffer is known to the compiler: addresses in LDS are a lane's own and a constant)
-    constexpr int BUF = decltype(buffer)::value;
+  auto arrived = [&] {   // every wave's part of this tile is there, and every wave is done with the buffer loaded next
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();   // every wave's part of this tile is there, and every wave is done with the buffer loaded next
+    __syncthreads();
+  };
+  // the tiles that every column sees whole (which buffer is known to the compiler: addresses in LDS are a lane's own and a constant) ..
+  const int whole_end = max(tile, min(end, s.n / KT));
+  int buf = 0;
+  auto tile_in = [&](auto buffer) __attribute__((always_inline)) {
+    constexpr int BUF = decltype(buffer)::value;
+    arrived();
     if (tile + 1 < end) load_tile(tile + 1, BUF ^ 1);
-    if (!idle) {
-      const char* kt = lds + BUF * 2 * TILE;
-      const int first = wk * SUB * 32, key = tile * KT + first;
-      if (key + 32 * SUB <= s.n) {
-        step(std::false_type{}, std::integral_constant<int, SUB>{}, kt, kt + TILE, first, key);
-      } else {
-#pragma unroll 1
-        for (int u = 0; u < 32 * SUB && key + u < s.n + s.rows; u += 32)
-          step(std::true_type{}, std::integral_constant<int, 1>{}, kt, kt + TILE, first + u, key + u);
-      }
-    }
+    const char* kt = lds + BUF * 2 * TILE;
+    step(std::false_type{}, std::integral_constant<int, SUB>{}, kt, kt + TILE, wk * SUB * 32, 0);
     ++tile;
   };
-  while (tile < end) {
+  if (idle) {
+#pragma unroll 1
+    for (; tile < end; ++tile, buf ^= 1) {
+      arrived();
+      if (tile + 1 < end) load_tile(tile + 1, buf ^ 1);
+    }
+  }
+  while (tile < whole_end) {
     tile_in(std::integral_constant<int, 0>{});
-    if (tile < end) tile_in(std::integral_constant<int, 1>{});
+    if (tile == whole_end) { buf = 1; break; }
+    tile_in(std::integral_constant<int, 1>{});
+  }
+  // .. and those with rows of the tree (a loop of its own: its registers are not the other one's)
+#pragma unroll 1
+  for (; tile < end; ++tile, buf ^= 1) {
+    arrived();
+    if (tile + 1 < end) load_tile(tile + 1, buf ^ 1);
+    const char* kt = lds + buf * 2 * TILE;
+    const int first = wk * SUB * 32, key = tile * KT + first;
+#pragma unroll 1
+    for (int u = 0; u < 32 * SUB && key + u < s.n + s.rows; u += 32) step(std::true_type{}, std::integral_constant<int, 1>{}, kt, kt + TILE, first + u, key + u);
   }
 #pragma unroll
   for (int e = 0; e < ET; ++e) mfma_settle(acc[e]);
