@@ -10,6 +10,7 @@
 // Scores are formed as S^T = K Q^T in 32 x 32 tiles: a lane then holds 16 keys of one column, the running maximum and sum are a lane's own up
 // to one exchange of the wave's halves, and the weights are already the second operand of O^T += V^T P^T (the order in which keys are
 // summed is free, so both operands take the one that S^T has).  V^T comes out of LDS by transposing reads.
+#include <atomic>
 #include <type_traits>
 
 #include "common.h"
@@ -44,14 +45,16 @@ template <> struct AttnType<f16> {
 // How a call is cut: blocks of 32 rw columns, tiles of kt keys; split: the tiles of a column block are dealt out in chunks of a length
 // that gives about `target` workgroups in all, whatever the lengths are (the workgroups work it out: the host does not know them), each
 // leaves its maximum, sum and unnormalised output in a slot of the workspace, and tree_join_kernel adds them up.
+// Rules, by what both sides take (us in a graph).  Split arenas of more than 1024 rows: the second launch costs 3.5, and one workgroup takes 9 for 700 keys
+// of 16 heads (split 14), 1500 keys of two sequences of 8 heads 15.  Up to 32 columns on 128 keys a tile and four waves where a call is short (one token on
+// 224 keys 5.3, on 64 keys and two waves 6.5), on 64 and two where it is long and heads have 128 dims, so that two workgroups are on a compute unit
+// (65536 keys 92 / 78).  Chunks that fill the GPU once where the column blocks are fewer than three quarters of that, else twice as many, so that
+// long sequences are cut (16 long ragged trees 225, chunks that begin a second round, / 186).
 struct TreePlan {
   int rw, kw, kt, row_blocks, target, slots;
   bool split;
 };
-#ifndef SPLIT_TARGET
-#define SPLIT_TARGET 512
-#endif
-constexpr int kSplitTarget = SPLIT_TARGET;
+constexpr int kSplitTarget = 512;   // workgroups that run at once: two a compute unit
 // The workspace of a split call: tiles of a chunk, the first slot of every sequence (written by the first workgroup for tree_join_kernel); the slots.
 __host__ __device__ static constexpr size_t tree_head_ints(int B) { return ((size_t)B + 1 + 63) / 64 * 64; }
 static TreePlan tree_plan(const TreeAttnArgs& a) {
@@ -563,7 +566,7 @@ template <class E, int DH, int RW, int KW, int SUB>
 static hipError_t tree_launch(hipStream_t st, const TreeAttnArgs& a, const TreePlan& p) {
   constexpr int tiles = 4 * 32 * KW * SUB * DH * 2, join = KW > 1 ? RW * KW * 32 * (DH + 4) * 4 : 0, bytes = tiles > join ? tiles : join;
   const auto kernel = tree_attn_kernel<E, DH, RW, KW, SUB>;
-  static bool ready[64];   // (of each GPU; setting it twice does no harm)
+  static std::atomic<bool> ready[64];   // (of each GPU; setting it twice does no harm)
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;

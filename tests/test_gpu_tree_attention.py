@@ -31,7 +31,7 @@ def cache(gen, layout, B, Hkv, cap, dh, dtype):
 def bound(out, mag, dots, dtype, n_seen):
     """Weights are rounded to the element type once (half a step of it on every p |v|), the result once; fp32 sums of dh products, exp2, and
     sums over the keys add steps of 2^-24: dh + 4 of them on a score, one a key (pairwise or not) on the sums.  fp16 keeps weights
-    down to 2^-39 of the largest (half of a smallest step for each key); its own smallest step is 2^-24."""
+    in steps of 2^-37 of the largest (half a step for each key); its own smallest step is 2^-24."""
     half = torch.finfo(DT[dtype]).eps / 2
     score = (132 * dots + 4)[..., None] * 2.0 ** -24
     tol = half * (mag + np.abs(out)) * (1 + 2.0 ** -6) + mag * (2 * score + 2.0 ** -24 * (n_seen + 8))
@@ -96,6 +96,13 @@ CASES = [   # dtype, layout, B, T, H, Hkv, dh, cached, masks, rows
     ("f16", "rows", 1, 1, 8, 1, 64, [4097], "chain", None),
     ("bf16", "rows", 1, 5, 4, 4, 128, [5000], "tree", None),
     ("bf16", "heads", 3, 1, 4, 4, 64, [1500, 3, 2300], "chain", None),
+    # long caches, whose work is split: more sequences than a wave has lanes, several column blocks, columns in twos and fours of 32, many chunks
+    ("bf16", "rows", 70, 3, 2, 2, 64, [37 * i % 1300 for i in range(70)], "tree", [i % 4 for i in range(70)]),
+    ("f16", "heads", 66, 1, 8, 8, 64, [0] * 60 + [1100, 64, 63, 1, 128, 700], "chain", None),
+    ("f16", "heads", 3, 64, 8, 1, 128, [1500, 0, 2900], "tree", [64, 9, 40]),
+    ("bf16", "rows", 2, 40, 3, 3, 64, [1100, 2000], "all", None),
+    ("f16", "rows", 1, 2, 16, 2, 128, [20000], "tree", None),
+    ("bf16", "heads", 1, 64, 6, 1, 64, [1999], "empty", None),
 ]
 
 
