@@ -20,6 +20,7 @@ namespace sd {
 
 typedef unsigned long long u64;
 constexpr int kBuckets = 2048, kList = 1024;
+constexpr int kShort = 512, kFew = 256;   // tokens that top-k looks among, and k at most, where it sorts them
 constexpr double kOne = (double)(1ull << 38);   // (at most 2^24 tokens: sums stay below 2^62)
 
 // Logits as whole numbers of the same order.
@@ -126,6 +127,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       if (r < rounds) held[r] = load(r);
   }
   for (int i = tid; i < kBuckets; i += THREADS) mass[i] = 0;
+  if (tid == 0) list_n = 0;
   float top = kNegInf;
   bool inf_top = false;   // only the infinite ones count: as zeros among -inf
   auto values = [&](Raw raw, float (&v)[VEC]) {
@@ -204,8 +206,29 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     if (k <= THREADS / 16) { m = fmaxf(m, dpp_f<kDppHalfMirror>(m)); m = fmaxf(m, dpp_f<kDppMirror>(m)); }
     among = m;
   }
+  const bool few_k = k > 1 && k <= kFew && k < V;
+  if (few_k) list[tid] = top;   // (the lane's own)
   block_range(top, among);
   if (among == -kNegInf) among = kNegInf;
+  if (few_k) {   // closer, by one wave: by halves between that and the largest, a value that k lanes still reach
+    if (wave == 0) {
+      float lo = among, hi = top, of[WAVES];
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) of[i] = list[i * 64 + lane];
+#pragma unroll 1
+      for (int turn = 0; turn < 8; ++turn) {
+        const float mid = lo + (hi - lo) * 0.5f;
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) c += __builtin_popcountll(__builtin_amdgcn_ballot_w64(of[i] >= mid));
+        if (c >= k) lo = mid; else hi = mid;
+      }
+      if (lane == 0) end.value = lo;
+    }
+    __syncthreads();
+    among = end.value;
+  }
+
   if (top == kNegInf) {   // nothing to draw from
     if (tid == 0) { a.token[row] = -1; if (a.logprob) a.logprob[row] = kNegInf; }
     return;
@@ -281,6 +304,80 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     const float steps = fminf((float)(kBuckets - 1) / (27.1f * temperature), 1e38f);   // (2^-39 = exp(-27.03): what is beyond weighs nothing)
     const float floor_k = fmaxf(by_p ? floor_0 : floor_x, by_k && !inf_top ? among : kNegInf);   // (what min-p drops counts for top-p)
     auto bucket = [&](float x) { return (int)fminf((top - x) * steps, (float)(kBuckets - 1)); };
+    // Few of many: the tokens that top-k looks among, put in their order (each counts the ones before it); all the rest is done on them alone.
+    // (One row of 32768 with top-k 50 and top-p: 19.6 us by the steps below, 11.6 so.)
+    if (by_k && few_k) {
+      int* list_i = reinterpret_cast<int*>(list_w);
+      all([&](int r, float (&v)[VEC]) {
+        if (!any(v, [&](float x) { return x >= floor_k; })) return;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (v[e] >= floor_k) {
+            const unsigned at = atomicAdd(&list_n, 1u);
+            if (at < kShort) { list[at] = v[e]; list_i[at] = first + (r * 64 + lane) * VEC + e; }
+          }
+      });
+      __syncthreads();
+      const int n = (int)list_n;
+      if (n <= kShort) {
+        constexpr int SHARE = THREADS / kShort;   // lanes of a token: each looks at a part of the others
+        static_assert(SHARE == 1 || SHARE == 2, "");
+        const int mine = tid / SHARE;
+        float x = kNegInf;
+        int xi = 0, rank = 0;
+        if (mine < n) {
+          x = list[mine];
+          xi = list_i[mine];
+          for (int j = tid % SHARE; j < n; j += SHARE) {
+            const float y = list[j];
+            rank += y > x || (y == x && list_i[j] < xi);
+          }
+        }
+        if (SHARE == 2) rank += dpp_i<kDppSwap1>(rank);
+        float* order_x = reinterpret_cast<float*>(mass);
+        int* order_i = reinterpret_cast<int*>(mass) + kShort;
+        u64* order_w = mass + kShort;
+        __syncthreads();   // (mass: cleared before, read by none)
+        if (mine < n && tid % SHARE == 0 && rank < k) { order_x[rank] = x; order_i[rank] = xi; }
+        __syncthreads();
+        const int m = min(n, k);
+        u64 w = 0;
+        if (tid < m) { w = weight(order_x[tid]); order_w[tid] = w; }
+        const u64 upto = scan_u64(w);
+        if (lane == 63) red[1][wave] = upto;
+        __syncthreads();
+        u64 before = upto - w, Z = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) { before += i < wave ? red[1][i] : 0; Z += red[1][i]; }
+        const u64 need = by_p ? (u64)ceil((double)p * (double)Z) : ~0ull;
+        const bool in = tid < m && (tid == 0 || (before < need && w >= least));
+        const u64 kept_w = sum_u64(in ? w : 0), kept_n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
+        if (lane == 0) { red[2][wave] = kept_w; red[3][wave] = kept_n; }
+        __syncthreads();
+        int kept = 0;
+        Z = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) { Z += red[2][i]; kept += (int)red[3][i]; }
+        // in the order of the vocabulary: the sum before a token, by THREADS / kFew lanes of it
+        constexpr int LANES = THREADS / kFew;
+        const int t = tid / LANES;
+        u64 below = 0;
+        int ti = 0;
+        if (t < kept) {
+          ti = order_i[t];
+          for (int j = tid % LANES; j < kept; j += LANES) below += order_i[j] < ti ? order_w[j] : 0;
+        }
+        below += dpp_u64<kDppSwap1>(below);
+        if (LANES == 4) below += dpp_u64<kDppSwap2>(below);
+        const double at = (double)a.u[row] * (double)Z;
+        const u64 target = at > 0.0 ? (at < (double)Z ? min((u64)at, Z - 1) : Z - 1) : 0;   // (as below)
+        if (t < kept && tid % LANES == 0 && below <= target && target < below + order_w[t]) {
+          a.token[row] = ti;
+          if (a.logprob) a.logprob[row] = (float)(((double)order_x[t] - (double)top) * inv_t - log((double)Z / kOne));
+        }
+        return;
+      }
+    }
     // the step in which the running sum reaches `need`, behind a barrier; false: none does
     auto locate = [&](u64 need) {
       u64 n[EACH], sum = 0;
