@@ -12,15 +12,19 @@
 // A workgroup a row, which is read once and stays in registers where it fits; every wave owns a consecutive part of it, so that the order
 // of the vocabulary is the order of the waves.  The end of top-k and of top-p is found without sorting: logits are counted (or weighed) in
 // kBuckets equal steps of max - x over the range in which weights are above zero, and the one step that holds the end is settled
-// among its own tokens.  Weights are formed where something depends on them: of all tokens only for top-p alone and for a plain draw.
+// among its own tokens.  Few tokens that stay are sorted instead, and all the rest is done on them alone.
+// Weights are formed where something depends on them: of all tokens only for top-p alone and for a plain draw.
 #include "common.h"
 #include "kernels.h"
 
 namespace sd {
 
 typedef unsigned long long u64;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kBuckets = 2048, kList = 1024;
-constexpr int kShort = 512, kFew = 256;   // tokens that top-k looks among, and k at most, where it sorts them
+// Tokens that stay are sorted where top-k or a count gives at most kFew of them, and what looks among them is at most kShort.  Sorting costs the
+// square of their number, the steps passes over the row: 1408 rows of 32768, top-k 120: 72 us sorted, 85 by steps; 200: 98 and 88 (96 rows of 131072: 28 and 59).
+constexpr int kFew = 192, kShort = 512;
 constexpr double kOne = (double)(1ull << 38);   // (at most 2^24 tokens: sums stay below 2^62)
 
 // Logits as whole numbers of the same order.
@@ -99,9 +103,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   constexpr int GROUP = HOLD > 9 ? 3 : 1, PARTS = HOLD > 0 ? (HOLD + GROUP - 1) / GROUP : 1;   // rounds whose sums a lane keeps as one
   typedef E Vec __attribute__((ext_vector_type(VEC)));
   typedef unsigned Raw __attribute__((ext_vector_type(4)));
-  __shared__ u64 mass[kBuckets];      // (of counts, where the end of top-k is looked for)
-  __shared__ float list[kList];
-  __shared__ u64 list_w[kList];
+  __shared__ alignas(16) u64 mass[kBuckets];      // (of counts, where the end of top-k is looked for)
+  __shared__ alignas(16) float list[kList];
+  __shared__ alignas(16) u64 list_w[kList];
   __shared__ u64 red[4][WAVES];         // (a place for each use: none waits until another one has been read)
   __shared__ float red_f[2][WAVES];
   __shared__ unsigned list_n;
@@ -305,21 +309,23 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
     const float floor_k = fmaxf(by_p ? floor_0 : floor_x, by_k && !inf_top ? among : kNegInf);   // (what min-p drops counts for top-p)
     auto bucket = [&](float x) { return (int)fminf((top - x) * steps, (float)(kBuckets - 1)); };
     // Few of many: the tokens that top-k looks among, put in their order (each counts the ones before it); all the rest is done on them alone.
-    // (One row of 32768 with top-k 50 and top-p: 19.6 us by the steps below, 11.6 so.)
-    if (by_k && few_k) {
+    // (One row of 32768 with top-k 50 and top-p: 19.6 us by the steps below, 10.2 so.  Four others a read: one a read 11.6, and top-k 120 of 1408 rows 101 us for 72.)
+    // `lowest`: below it is none that stays; `most` tokens at most stay, and of them the first until the weights before one reach `need` (0: p of all these).
+    auto sorted = [&](float lowest, int most, u64 need) __attribute__((always_inline)) {
       int* list_i = reinterpret_cast<int*>(list_w);
       all([&](int r, float (&v)[VEC]) {
-        if (!any(v, [&](float x) { return x >= floor_k; })) return;
+        if (!any(v, [&](float x) { return x >= lowest; })) return;
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (v[e] >= floor_k) {
+          if (v[e] >= lowest) {
             const unsigned at = atomicAdd(&list_n, 1u);
             if (at < kShort) { list[at] = v[e]; list_i[at] = first + (r * 64 + lane) * VEC + e; }
           }
       });
       __syncthreads();
       const int n = (int)list_n;
-      if (n <= kShort) {
+      if (n > kShort) return false;
+      {
         constexpr int SHARE = THREADS / kShort;   // lanes of a token: each looks at a part of the others
         static_assert(SHARE == 1 || SHARE == 2, "");
         const int mine = tid / SHARE;
@@ -328,9 +334,11 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
         if (mine < n) {
           x = list[mine];
           xi = list_i[mine];
-          for (int j = tid % SHARE; j < n; j += SHARE) {
-            const float y = list[j];
-            rank += y > x || (y == x && list_i[j] < xi);
+          for (int j = 4 * (tid % SHARE); j < n; j += 4 * SHARE) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(list + j);
+            const i32x4 yi = *reinterpret_cast<const i32x4*>(list_i + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) rank += (j + e < n) & ((y[e] > x) | ((y[e] == x) & (yi[e] < xi)));
           }
         }
         if (SHARE == 2) rank += dpp_i<kDppSwap1>(rank);
@@ -338,9 +346,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
         int* order_i = reinterpret_cast<int*>(mass) + kShort;
         u64* order_w = mass + kShort;
         __syncthreads();   // (mass: cleared before, read by none)
-        if (mine < n && tid % SHARE == 0 && rank < k) { order_x[rank] = x; order_i[rank] = xi; }
+        if (mine < n && tid % SHARE == 0 && rank < most) { order_x[rank] = x; order_i[rank] = xi; }
         __syncthreads();
-        const int m = min(n, k);
+        const int m = min(n, most);
         u64 w = 0;
         if (tid < m) { w = weight(order_x[tid]); order_w[tid] = w; }
         const u64 upto = scan_u64(w);
@@ -349,7 +357,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
         u64 before = upto - w, Z = 0;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) { before += i < wave ? red[1][i] : 0; Z += red[1][i]; }
-        const u64 need = by_p ? (u64)ceil((double)p * (double)Z) : ~0ull;
+        if (need == 0) need = by_p ? (u64)ceil((double)p * (double)Z) : ~0ull;
         const bool in = tid < m && (tid == 0 || (before < need && w >= least));
         const u64 kept_w = sum_u64(in ? w : 0), kept_n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
         if (lane == 0) { red[2][wave] = kept_w; red[3][wave] = kept_n; }
@@ -358,26 +366,33 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
         Z = 0;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) { Z += red[2][i]; kept += (int)red[3][i]; }
-        // in the order of the vocabulary: the sum before a token, by THREADS / kFew lanes of it
-        constexpr int LANES = THREADS / kFew;
-        const int t = tid / LANES;
+        // in the order of the vocabulary: the sum before a token, by SHARE lanes of it
+        const int t = tid / SHARE;
         u64 below = 0;
         int ti = 0;
         if (t < kept) {
           ti = order_i[t];
-          for (int j = tid % LANES; j < kept; j += LANES) below += order_i[j] < ti ? order_w[j] : 0;
+          for (int j = 4 * (tid % SHARE); j < kept; j += 4 * SHARE) {
+            const i32x4 yi = *reinterpret_cast<const i32x4*>(order_i + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const u64 w = order_w[j + e];
+              below += ((j + e < kept) & (yi[e] < ti)) ? w : 0;
+            }
+          }
         }
-        below += dpp_u64<kDppSwap1>(below);
-        if (LANES == 4) below += dpp_u64<kDppSwap2>(below);
+        if (SHARE == 2) below += dpp_u64<kDppSwap1>(below);
         const double at = (double)a.u[row] * (double)Z;
         const u64 target = at > 0.0 ? (at < (double)Z ? min((u64)at, Z - 1) : Z - 1) : 0;   // (as below)
-        if (t < kept && tid % LANES == 0 && below <= target && target < below + order_w[t]) {
+        if (t < kept && tid % SHARE == 0 && below <= target && target < below + order_w[t]) {
           a.token[row] = ti;
           if (a.logprob) a.logprob[row] = (float)(((double)order_x[t] - (double)top) * inv_t - log((double)Z / kOne));
         }
-        return;
       }
-    }
+      return true;
+    };
+    auto lower_edge = [&](int step) { return top - ((float)step + 1.01f) / steps - 1e-6f * fabsf(top); };   // by more than the rounding of a bucket
+    if (by_k && few_k && sorted(floor_k, k, 0)) return;
     // the step in which the running sum reaches `need`, behind a barrier; false: none does
     auto locate = [&](u64 need) {
       u64 n[EACH], sum = 0;
@@ -403,7 +418,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       const int B = end.bucket;
       const u64 over = end.over;
       // (every value of the step, and few others: by more than the rounding of a bucket)
-      const float wide = 1e-6f * fabsf(top), from = fmaxf(floor_k, top - ((float)B + 1.01f) / steps - wide), to = top - ((float)B - 0.01f) / steps + wide;
+      const float wide = 1e-6f * fabsf(top), from = fmaxf(floor_k, lower_edge(B)), to = top - ((float)B - 0.01f) / steps + wide;
       all([&](int, float (&v)[VEC]) {
         if (!any(v, [&](float x) { return x >= from && x <= to; })) return;
 #pragma unroll
@@ -519,6 +534,24 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       }
       const u64 need = (u64)ceil((double)p * (double)block_sum(sum));
       if (locate(need)) {
+        if (!cut_k) {   // all before the end are above a lower edge, and often few: counted first (flat rows put thousands in a list for nothing)
+          const float lowest = fmaxf(floor_0, lower_edge(end.bucket));
+          unsigned many = 0;
+          all([&](int, float (&v)[VEC]) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) many += v[e] >= lowest;
+          });
+          const u64 mine = sum_u64(many);
+          if (lane == 0) red[2][wave] = mine;
+          __syncthreads();
+          u64 n = 0;
+#pragma unroll
+          for (int i = 0; i < WAVES; ++i) n += red[2][i];
+          if (n <= kFew) {   // (1408 rows of 32768, top-p 0.9: 79 us so, 101 without)
+            __syncthreads();   // (red[2] is written again)
+            if (sorted(lowest, kShort, need)) return;
+          }
+        }
         settle(need, true);
         const u64 w = end.w, ties = cut_k && end.value == cut ? equal : end.equal;
         equal = min(ties, (need - end.over + w - 1) / w);
