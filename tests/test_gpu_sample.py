@@ -126,3 +126,23 @@ def test_captured(ctx):
         torch.cuda.synchronize()
         sd.specdec_sample(ctx, logits, None, None, top_p, None, u, want)
         assert torch.equal(token, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [700, 20000, 150001])
+def test_how_many_stay(ctx, dtype, V):
+    """Rows where some number of heavy tokens, equal or not, hold nearly everything; top-k and top-p end within them, at their end and beyond."""
+    rng = np.random.default_rng(V)
+    for spread in (0.0, 1.0):
+        rows, k, p, u = [], [], [], []
+        for heavy in (1, 3, 127, 128, 129, 191, 192, 193, 194, 255, 256, 511, 512, 513, 600):
+            for top_k, top_p in ((0, 0.9), (0, 0.5), (heavy, 1.0), (heavy - 1, 0.9), (heavy + 1, 1.0), (192, 0.7), (193, 1.0)):
+                x = (rng.standard_normal(V) - 25).astype(np.float32)
+                x[rng.permutation(V)[:heavy]] = 4 + spread * rng.random(heavy)
+                rows.append(x)
+                k.append(top_k)
+                p.append(top_p)
+                u.append(rng.random())
+        n = len(rows)
+        logits = torch.tensor(np.stack(rows)).to(DT[dtype]).cuda()
+        check(ctx, logits, np.full(n, 1, np.float32), np.array(k, np.int32), np.array(p, np.float32), None, np.array(u, np.float32))
