@@ -1426,6 +1426,8 @@ int verify_impl(specdec_ctx* c, const int32_t* draft, int32_t k, int32_t beta, f
   hipStream_t st = S(stream);
   const int B = c->B, T = k + 1, R = B * T;
   const bool small = skinny_ok(c, m, R, T);
+  if (small && (m.fp8 || m.kv8) && (c->resident || c->sliced))
+    return fail(c, SPECDEC_ERR_BAD_STATE, "a model bound with FP8 weights or FP8 cross keys/values runs small passes on the default kernels only");
   // The fused small-batch decoder kernels, whose every block redoes what precedes its product and which embed the rows
   // themselves, where that is little: one sequence of few rows, d = 512 (3 rows 184 against 205 us, 11: 210 / 214, 16: 220 /
   // 218; two sequences of 6 235 / 214; d = 1024: 6 rows 285 / 268, 26 521 / 302).  Otherwise the general ones.
@@ -1443,6 +1445,7 @@ int verify_impl(specdec_ctx* c, const int32_t* draft, int32_t k, int32_t beta, f
     HIPCHK(c, sd::skinny_init(m.d.d_model));
     m.skinny_ready = true;
   }
+  c->last_T = c->last_tree = 0;   // (refused above: the pass before stays to be committed; from here on its drafts are overwritten)
   if (fused)
     LAUNCH(c, SPECDEC_KIND_OTHER, st, sd::assemble_verify(st, c->st, m.rm, draft, B, k, m.d.vocab));
   else
@@ -1452,8 +1455,6 @@ int verify_impl(specdec_ctx* c, const int32_t* draft, int32_t k, int32_t beta, f
   const unsigned* failed = one ? persist_flags(c->way, m) + 1 : nullptr;
   float* sums = one ? m.skp : m.x;   // the last residual sums (the one-kernel decoder keeps its input rows)
   int n_tiles = (m.d.vocab + 63) / 64;   // per-row partial records of the vocabulary kernel that ran
-  if (small && (m.fp8 || m.kv8) && (c->resident || c->sliced))
-    return fail(c, SPECDEC_ERR_BAD_STATE, "a model bound with FP8 weights or FP8 cross keys/values runs small passes on the default kernels only");
   if (small) {
     sd::SkSrc fin{};
     if (!fused) {
@@ -1483,7 +1484,6 @@ int verify_impl(specdec_ctx* c, const int32_t* draft, int32_t k, int32_t beta, f
   LAUNCH(c, SPECDEC_KIND_ACCEPT, st, sd::merge_accept(st, vs.part, vs.zd, n_tiles, vs.row_stats, c->st, B, k, beta, tau, m.d.pad_id,
                                       accept_len, next_token, failed));
   c->last_T = k + 1;
-  c->last_tree = 0;
   c->last_row_stats = vs.row_stats;
   return SPECDEC_OK;
 }
