@@ -320,6 +320,10 @@ int specdec_commit_tree(specdec_ctx* ctx, const int32_t* token, int32_t* accept_
  * not yet committed, draft statistics and encoder memories (specdec_get_memory) do not outlive it. */
 int specdec_fork(specdec_ctx* ctx, const int32_t* src, int32_t B, void* stream);
 
+/* Sizes that the buffers of the calls above go by, for callers that check theirs (host values, nullable): sequences of the present batch,
+ * rows a sequence (n + 1) of the pass over trees that specdec_commit_tree would commit, the verifier's vocabulary; 0 where there is none. */
+int specdec_pass_sizes(const specdec_ctx* ctx, int32_t* batch, int32_t* tree_rows, int32_t* vocab);
+
 /* Roll sequences back: j_b <- min(j_b, len[b]) (len device int32 [B]); cached lengths are cut
  * to match and a sequence whose j drops below its cap is unfinished again.  Like the
  * rollback inside commit this moves no data: rows beyond j are simply dead. */

@@ -99,6 +99,7 @@ EXPORTS = {
     "specdec_verify_tree": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
     "specdec_commit_tree": (C.c_int, [C.c_void_p] * 6),
     "specdec_fork": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
+    "specdec_pass_sizes": (C.c_int, [C.c_void_p] + [C.POINTER(C.c_int32)] * 3),
     "specdec_tree_attention_bytes": (C.c_int, [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]),
     "specdec_tree_attention": (C.c_int, [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]),
     "specdec_tree_visible": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
@@ -279,17 +280,39 @@ def specdec_commit(ctx, accept_len, next_token, n_active=None):
     _check(ctx, lib().specdec_commit(ctx, _ptr(accept_len), _ptr(next_token), _ptr(n_active), _stream()))
 
 
+def specdec_pass_sizes(ctx):
+    """(sequences of the present batch, rows a sequence of the pass over trees that can be committed, the verifier's vocabulary), 0 where there is none."""
+    n = [C.c_int32() for _ in range(3)]
+    _check(ctx, lib().specdec_pass_sizes(ctx, *[C.byref(x) for x in n]))
+    return tuple(x.value for x in n)
+
+
 def specdec_verify_tree(ctx, draft, parent, logits):
     """draft, parent int32 [B, n] (None: n = 0); logits fp32 [B, n + 1, V]."""
-    _check(ctx, lib().specdec_verify_tree(ctx, _ptr(draft), _ptr(parent), 0 if draft is None else draft.shape[1], _ptr(logits), _stream()))
+    B, _, V = specdec_pass_sizes(ctx)
+    d, z = (0, 0) if draft is None else _shape("draft", draft, 2), _shape("logits", logits, 3)
+    # (without a batch or a model: by the tensors' own sizes, and the library says what is missing)
+    B, n, V = B or d[0] or z[0], d[1], V or z[2]
+    if n and parent is None:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, "parent: None, with drafts")
+    dp, pp = _ints("draft", draft, (B, n)), _ints("parent", parent, (B, n))
+    _check(ctx, lib().specdec_verify_tree(ctx, dp, pp, n, _ints("logits", logits, (B, n + 1, V), "float32"), _on_gpu(draft, parent, logits)))
 
 
 def specdec_commit_tree(ctx, token, accept_len=None, next_token=None, n_active=None):
-    _check(ctx, lib().specdec_commit_tree(ctx, _ptr(token), _ptr(accept_len), _ptr(next_token), _ptr(n_active), _stream()))
+    """token int32 [B, n + 1] of the latest specdec_verify_tree; accept_len, next_token int32 [B] or None, n_active int32 [1] or None."""
+    B, T, _ = specdec_pass_sizes(ctx)
+    t = _shape("token", token, 2)
+    B, T = B or t[0], T or t[1]
+    args = (_ints("token", token, (B, T)), _ints("accept_len", accept_len, (B,)), _ints("next_token", next_token, (B,)),
+            None if n_active is None else _ints("n_active", n_active.view(-1), (1,)))
+    _check(ctx, lib().specdec_commit_tree(ctx, *args, _on_gpu(token, accept_len, next_token, n_active)))
 
 
 def specdec_fork(ctx, src):
-    _check(ctx, lib().specdec_fork(ctx, _ptr(src), src.numel(), _stream()))
+    """src int32 [sequences of the new batch]."""
+    n = _shape("src", src, 1)
+    _check(ctx, lib().specdec_fork(ctx, _ints("src", src, n), n[0], _on_gpu(src)))
 
 
 def specdec_rewind(ctx, length):
@@ -362,6 +385,13 @@ def _ints(name: str, t, shape, of="int32"):
     if t.shape != shape or t.dtype is not getattr(torch, of) or not t.is_contiguous():
         raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: contiguous {of} {list(shape)} expected, not {t.dtype} {list(t.shape)}")
     return t.data_ptr()
+
+
+def _shape(name: str, t, dims: int):
+    """Its sizes, if it has that many dimensions."""
+    if t is None or t.dim() != dims:
+        raise SpecDecError(SPECDEC_ERR_INVALID_ARG, f"{name}: {dims} dimensions expected, not {None if t is None else list(t.shape)}")
+    return tuple(t.shape)
 
 
 def _strided(name: str, t, shape):

@@ -1671,6 +1671,14 @@ int specdec_fork(specdec_ctx* c, const int32_t* src, int32_t B_new, void* stream
   return SPECDEC_OK;
 }
 
+int specdec_pass_sizes(const specdec_ctx* c, int32_t* batch, int32_t* tree_rows, int32_t* vocab) {
+  if (!c) return SPECDEC_ERR_INVALID_ARG;
+  if (batch) *batch = c->B;
+  if (tree_rows) *tree_rows = c->last_tree;
+  if (vocab) *vocab = c->m[SPECDEC_VERIFIER].bound ? c->m[SPECDEC_VERIFIER].d.vocab : 0;
+  return SPECDEC_OK;
+}
+
 int specdec_rewind(specdec_ctx* c, const int32_t* len, void* stream) {
   if (!c) return SPECDEC_ERR_INVALID_ARG;
   if (!c->state_bound || c->B <= 0) return fail(c, SPECDEC_ERR_BAD_STATE, "begin not called");
