@@ -14,6 +14,8 @@
 // kBuckets equal steps of max - x over the range in which weights are above zero, and the one step that holds the end is settled
 // among its own tokens.  Few tokens that stay are sorted instead, and all the rest is done on them alone.
 // Weights are formed where something depends on them: of all tokens only for top-p alone and for a plain draw.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -637,11 +639,22 @@ static void sample_launch(hipStream_t st, const SampleArgs& a) {
   else hipLaunchKernelGGL((sample_kernel<E, 16, 0>), dim3(a.rows), dim3(1024), 0, st, a);
 }
 
-hipError_t sample(hipStream_t st, const SampleArgs& a) {
-  if (a.dtype == 0) sample_launch<float>(st, a);
-  else if (a.dtype == 1) sample_launch<bf16>(st, a);
-  else sample_launch<f16>(st, a);
-  return hipGetLastError();
+// (a grid has fewer than 2^32 threads in a dimension: 2^21 rows of up to 1024 threads a launch)
+hipError_t sample(hipStream_t st, const SampleArgs& all) {
+  constexpr int most = 1 << 21;
+  for (int r0 = 0; r0 < all.rows; r0 += std::min(most, all.rows - r0)) {
+    SampleArgs a = all;
+    a.rows = std::min(most, all.rows - r0);
+    a.logits = static_cast<const char*>(all.logits) + r0 * all.row_stride * (all.dtype == 0 ? 4 : 2);
+    auto from = [r0](auto& p) { if (p) p += r0; };
+    from(a.temperature); from(a.top_k); from(a.top_p); from(a.min_p); from(a.u); from(a.token); from(a.logprob);
+    if (a.dtype == 0) sample_launch<float>(st, a);
+    else if (a.dtype == 1) sample_launch<bf16>(st, a);
+    else sample_launch<f16>(st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace sd

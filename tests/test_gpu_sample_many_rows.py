@@ -90,3 +90,22 @@ def test_every_place_of_a_row(ctx, dtype, V, rows):
         near = np.minimum(np.abs(target - sums[np.maximum(want - 1, 0)]), np.abs(sums[want] - target)) <= V
         differ = token.cpu().numpy() != want
         assert not np.any(differ & ~near), (part, np.flatnonzero(differ & ~near)[:5])
+
+
+@pytest.mark.parametrize("rows", [(1 << 21) + 1, (1 << 23) + 5])
+def test_more_rows_than_a_launch_takes(ctx, rows):
+    """Short rows by the million: greedy ones against arg-max, drawn ones against the same rows in smaller calls."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((rows, 5), generator=gen, device="cuda").to(torch.bfloat16)[:, :3]
+    u = torch.rand(rows, generator=gen, device="cuda")
+    t = torch.rand(rows, generator=gen, device="cuda") + 0.5
+    k = torch.randint(0, 4, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    token, _ = draw(ctx, x, [torch.zeros_like(t), None, None, None, u])
+    greatest = x.float().amax(1, keepdim=True)
+    assert torch.equal(token.long(), torch.where(x.float() == greatest, torch.arange(3, device="cuda"), 3).amin(1))
+    cols = [t, k, torch.full_like(t, 0.9), torch.full_like(t, 0.05), u]
+    token, logprob = draw(ctx, x, cols)
+    for a in (0, (1 << 21) - 1000, (1 << 22) - 10, rows - 1500):
+        a = min(a, rows - 1500)
+        some, lp = draw(ctx, x[a:a + 1500], [c[a:a + 1500] for c in cols])
+        assert torch.equal(token[a:a + 1500], some) and torch.equal(logprob[a:a + 1500], lp), a
