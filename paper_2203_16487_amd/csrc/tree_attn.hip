@@ -611,8 +611,14 @@ __global__ __launch_bounds__(64) void tree_visible_kernel(const int* __restrict_
   if (lane <= n) visible[(size_t)b * (n + 1) + lane] = mask[lane];
 }
 hipError_t tree_visible(hipStream_t st, const int* parent, int B, int n, u64* visible) {
-  hipLaunchKernelGGL(tree_visible_kernel, dim3(B), dim3(64), 0, st, parent, n, visible);
-  return hipGetLastError();
+  constexpr int most = 1 << 24;   // (a grid has fewer than 2^32 threads in a dimension)
+  for (int b0 = 0, now; b0 < B; b0 += now) {
+    now = B - b0 < most ? B - b0 : most;
+    hipLaunchKernelGGL(tree_visible_kernel, dim3(now), dim3(64), 0, st, parent + (size_t)b0 * n, n, visible + (size_t)b0 * (n + 1));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace sd
