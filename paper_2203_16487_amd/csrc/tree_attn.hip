@@ -499,8 +499,7 @@ __global__ __launch_bounds__(JW == 1 ? 256 : 64 * JW) void tree_join_kernel(Tree
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cols = 32 * p.rw, G = a.H / a.Hkv;
   int id = blockIdx.x;
   const int c = id % (cols / COLS) * COLS + (JW == 1 ? wave : 0); id /= cols / COLS;
-  const int block = id % p.row_blocks; id /= p.row_blocks;
-  const int hk = id % a.Hkv, b = id / a.Hkv;
+  const int block = id % p.row_blocks, hk = id / p.row_blocks, b = blockIdx.y;
   const int* head = reinterpret_cast<const int*>(a.ws);
   const int per = head[0], first = head[1 + b];
   const TreeSeq s = tree_seq(a, p, b);
@@ -579,9 +578,10 @@ static hipError_t tree_launch(hipStream_t st, const TreeAttnArgs& a, const TreeP
   e = hipGetLastError();
   if (e != hipSuccess || !p.split) return e;
   // (a column has about as many chunks as the target is larger than the number of column blocks)
-  const unsigned columns = (unsigned)a.B * a.Hkv * p.row_blocks * 32 * p.rw;
-  if (p.target <= 8 * a.B * a.Hkv * p.row_blocks) hipLaunchKernelGGL((tree_join_kernel<E, DH / 64, 1>), dim3(columns / 4), dim3(256), 0, st, a, p);
-  else hipLaunchKernelGGL((tree_join_kernel<E, DH / 64, 16>), dim3(columns), dim3(1024), 0, st, a, p);
+  // (sequences in y: columns of 64 - 1024 threads, batch x heads x rows of them, would pass the 2^32 threads of one dimension)
+  const unsigned columns = (unsigned)a.Hkv * p.row_blocks * 32 * p.rw;
+  if (p.target <= 8 * a.B * a.Hkv * p.row_blocks) hipLaunchKernelGGL((tree_join_kernel<E, DH / 64, 1>), dim3(columns / 4, a.B), dim3(256), 0, st, a, p);
+  else hipLaunchKernelGGL((tree_join_kernel<E, DH / 64, 16>), dim3(columns, a.B), dim3(1024), 0, st, a, p);
   return hipGetLastError();
 }
 
