@@ -419,7 +419,8 @@ int specdec_sample(specdec_ctx* ctx, const void* logits, specdec_dtype dtype, in
                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
                    int32_t* token, float* logprob, void* stream);
 
-/* Keys / values as slabs of rows, one per layer, sequence and head, k and v laid out alike. */
+/* Keys / values as slabs of rows, one per layer, sequence and head, k and v laid out alike.  Rows are moved in place, so none may lie in two of
+ * them: of layers, sequences, heads, rows, and k against v, each goes over a stride that is no less than what those of smaller strides cover. */
 typedef struct {
   int32_t layers, heads, capacity;   /* layers * heads at most 32767 */
   int32_t row_bytes;                 /* of a head's row, consecutive; a multiple of 16 */

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstdarg>
 #include <cstddef>
@@ -11,6 +12,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "../../include/specdec.h"
@@ -1816,6 +1818,26 @@ int attn_args(specdec_ctx* c, const specdec_tree_attn_desc* d, sd::TreeAttnArgs*
   return SPECDEC_OK;
 }
 
+// Whether some of these places of `extent` consecutive units may be the same ones: dimensions {count, stride} that are neither nested nor beside each
+// other, by order of their strides, count as such.
+template <size_t N>
+bool overlapping(std::array<std::pair<int64_t, int64_t>, N> dims, int64_t extent) {
+  std::sort(dims.begin(), dims.end(), [](const auto& a, const auto& b) { return a.second < b.second; });
+  double end = (double)extent;   // (beyond 2^53 far more than any memory)
+  for (const auto& [count, stride] : dims) {
+    if (count < 2) continue;
+    if ((double)stride < end) return true;
+    end += (double)(count - 1) * (double)stride;
+  }
+  return false;
+}
+
+// Moves write: no row may lie in two places of `seqs` sequences of k and v.
+bool slabs_overlap(const sd::CacheSlabs& s, int seqs) {
+  const int64_t apart = s.v ? std::llabs(static_cast<const char*>(s.v) - static_cast<const char*>(s.k)) : 0;
+  return overlapping<5>({{{s.layers, s.layer_s}, {seqs, s.seq_s}, {s.heads, s.head_s}, {s.capacity, s.row_s}, {s.v ? 2 : 1, apart}}}, s.row_bytes);
+}
+
 int slab_args(specdec_ctx* c, const specdec_cache_desc* d, void* k, void* v, sd::CacheSlabs* s) {
   if (!c) return SPECDEC_ERR_INVALID_ARG;
   if (!d || !k) return fail(c, SPECDEC_ERR_INVALID_ARG, "null desc/k");
@@ -1893,6 +1915,7 @@ int specdec_fork_cache(specdec_ctx* c, const specdec_cache_desc* d, void* k, voi
   if (B < 1 || B > 4096 || n_src < 1 || n_src > 4096) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d, n_src = %d outside [1, 4096]", B, n_src);
   if ((int64_t)s.capacity * (s.row_bytes / 16) * s.heads >= (int64_t)1 << 31)
     return fail(c, SPECDEC_ERR_TOO_LARGE, "capacity x heads x row_bytes of a layer reaches 32 GiB");
+  if (slabs_overlap(s, std::max(B, n_src))) return fail(c, SPECDEC_ERR_INVALID_ARG, "layers, sequences, heads, rows, or k and v overlap");
   HIPCHK(c, sd::cache_fork(S(stream), s, B, n_src, src, len));
   return SPECDEC_OK;
 }
@@ -1905,6 +1928,7 @@ int specdec_compact_cache(specdec_ctx* c, const specdec_cache_desc* d, void* k, 
   if (!first || !path || !count) return fail(c, SPECDEC_ERR_INVALID_ARG, "null first/path/count");
   if (B < 1 || B > 65535 || n < 1 || n > sd::kCompactRows) return fail(c, SPECDEC_ERR_INVALID_ARG, "B = %d, n = %d (1 .. %d)", B, n, sd::kCompactRows);
   if (s.row_bytes > sd::kCompactRowBytes) return fail(c, SPECDEC_ERR_INVALID_ARG, "row_bytes = %d exceeds %d", s.row_bytes, sd::kCompactRowBytes);
+  if (slabs_overlap(s, B)) return fail(c, SPECDEC_ERR_INVALID_ARG, "layers, sequences, heads, rows, or k and v overlap");
   HIPCHK(c, sd::cache_compact(S(stream), s, B, n, first, path, count));
   return SPECDEC_OK;
 }
