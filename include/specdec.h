@@ -386,7 +386,8 @@ typedef struct {
   int32_t head_dim;              /* 64 or 128 */
   int32_t capacity;
   float scale;
-  /* elements between two sequences, rows and heads, multiples of 8, not negative (0: shared); a head's values are consecutive */
+  /* elements between two sequences, rows and heads, multiples of 8, not negative (0: shared); a head's values are consecutive.
+   * Of out each goes over a stride that is no less than what those of smaller strides cover: nothing is written twice. */
   int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
 } specdec_tree_attn_desc;
 /* Bytes of (device) workspace that the call needs, 256-byte aligned; its contents do not matter before or after.  Calls that may

@@ -1791,6 +1791,20 @@ namespace {
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// Whether some of these places of `extent` consecutive units may be the same ones: dimensions {count, stride} that are neither nested nor beside each
+// other, by order of their strides, count as such.
+template <size_t N>
+bool overlapping(std::array<std::pair<int64_t, int64_t>, N> dims, int64_t extent) {
+  std::sort(dims.begin(), dims.end(), [](const auto& a, const auto& b) { return a.second < b.second; });
+  double end = (double)extent;   // (beyond 2^53 far more than any memory)
+  for (const auto& [count, stride] : dims) {
+    if (count < 2) continue;
+    if ((double)stride < end) return true;
+    end += (double)(count - 1) * (double)stride;
+  }
+  return false;
+}
+
 int attn_args(specdec_ctx* c, const specdec_tree_attn_desc* d, sd::TreeAttnArgs* a) {
   if (!c) return SPECDEC_ERR_INVALID_ARG;
   if (!d) return fail(c, SPECDEC_ERR_INVALID_ARG, "null desc");
@@ -1807,29 +1821,14 @@ int attn_args(specdec_ctx* c, const specdec_tree_attn_desc* d, sd::TreeAttnArgs*
   for (const int64_t* s : strides)
     for (int i = 0; i < 3; ++i)
       if (s[i] < 0 || s[i] % 8 || s[i] > (int64_t(1) << 40)) return fail(c, SPECDEC_ERR_INVALID_ARG, "stride %lld: not a multiple of 8, negative or too large", (long long)s[i]);
-  const int64_t many[3] = {d->batch, d->rows, d->n_heads};
-  for (int i = 0; i < 3; ++i)
-    if (many[i] > 1 && d->out_stride[i] < d->head_dim) return fail(c, SPECDEC_ERR_INVALID_ARG, "rows of out overlap");
+  if (overlapping<3>({{{d->batch, d->out_stride[0]}, {d->rows, d->out_stride[1]}, {d->n_heads, d->out_stride[2]}}}, d->head_dim))
+    return fail(c, SPECDEC_ERR_INVALID_ARG, "rows of out overlap");
   *a = sd::TreeAttnArgs{};
   for (int i = 0; i < 3; ++i) { a->q_s[i] = d->q_stride[i]; a->k_s[i] = d->k_stride[i]; a->v_s[i] = d->v_stride[i]; a->o_s[i] = d->out_stride[i]; }
   a->scale = d->scale;
   a->B = d->batch; a->T = d->rows; a->H = d->n_heads; a->Hkv = d->n_kv_heads; a->dh = d->head_dim; a->cap = d->capacity;
   a->f16 = d->dtype == SPECDEC_F16;
   return SPECDEC_OK;
-}
-
-// Whether some of these places of `extent` consecutive units may be the same ones: dimensions {count, stride} that are neither nested nor beside each
-// other, by order of their strides, count as such.
-template <size_t N>
-bool overlapping(std::array<std::pair<int64_t, int64_t>, N> dims, int64_t extent) {
-  std::sort(dims.begin(), dims.end(), [](const auto& a, const auto& b) { return a.second < b.second; });
-  double end = (double)extent;   // (beyond 2^53 far more than any memory)
-  for (const auto& [count, stride] : dims) {
-    if (count < 2) continue;
-    if ((double)stride < end) return true;
-    end += (double)(count - 1) * (double)stride;
-  }
-  return false;
 }
 
 // Moves write: no row may lie in two places of `seqs` sequences of k and v.

@@ -35,3 +35,15 @@ def test_moves_in_place(ctx, change, k, v):
         assert sd.lib().specdec_compact_cache(ctx, C.byref(d), *kv, 4, P, P, 3, P, None) == BAD
         assert b"overlap" in sd.lib().specdec_last_error(ctx)
     assert sd.lib().specdec_fork_cache(ctx, C.byref(d), k, v, 2, P, 4, P, None) == BAD       # (sources count, too)
+
+
+@pytest.mark.parametrize("stride,fine", [((2048, 512, 64), True), ((512, 1024, 64), True), ((64, 128, 512), True), ((2048, 448, 64), False), ((2048, 64, 64), False), ((1984, 512, 64), False),
+                                         ((64, 2048, 512), False), ((0, 512, 64), False), ((2048, 512, 0), False)])
+def test_attention_output(ctx, stride, fine):
+    """Two sequences of four rows of eight heads of 64."""
+    s = lambda x: (C.c_int64 * 3)(*x)
+    d = sd.specdec_tree_attn_desc(sd.SPECDEC_BF16, 2, 4, 8, 2, 64, 100, 0.125, s((0, 0, 0)), s((0, 0, 0)), s((0, 0, 0)), s(stride))
+    n = C.c_size_t()
+    assert sd.lib().specdec_tree_attention_bytes(ctx, C.byref(d), C.byref(n)) == (sd.SPECDEC_OK if fine else BAD)
+    if not fine:
+        assert b"overlap" in sd.lib().specdec_last_error(ctx)
