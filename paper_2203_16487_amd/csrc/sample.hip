@@ -245,7 +245,10 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   const double inv_t = 1.0 / (double)temperature, per_x = fmax(inv_t * 1.44269504088896340736, 1e-300);
   const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * kOne) : 0;
   // below floor_0 nothing weighs anything, below floor_x not `least`, by margins far beyond the rounding of these lines
-  auto floor_of = [&](float nats) { return fmaxf(top - 1.0001f * temperature * (nats + 1e-4f) - 1e-6f * fabsf(top), -3.402823466e38f); };
+  // (in 64 bits: the product passes the largest fp32 for temperatures from 1e37, which logits of the type's range can need)
+  auto floor_of = [&](float nats) {
+    return (float)fmax((double)top - 1.0001 * (double)temperature * ((double)nats + 1e-4) - 1e-6 * fabs((double)top), -3.4028234663852886e38);
+  };
   auto nats_of = [](float w) { return 0.6931472f * (38.f - __builtin_amdgcn_logf(w)); };   // from the largest down to a weight
   const float floor_0 = floor_of(27.1f), floor_x = least > 0 ? floor_of(nats_of((float)least)) : floor_0;
   const double weightless = -46.0 / per_x;
@@ -307,7 +310,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
   bool some = alone;   // not all of those equal to it
   const bool by_k = !alone && k > 0 && k < V, by_p = !alone && p < 1.f;
   if (by_k || by_p) {
-    const float steps = fminf((float)(kBuckets - 1) / (27.1f * temperature), 1e38f);   // (2^-39 = exp(-27.03): what is beyond weighs nothing)
+    // (2^-39 = exp(-27.03): what is beyond weighs nothing.  Not 0 however large the temperature: a difference beyond fp32 is infinite, and in the last step)
+    const float steps = fmaxf(fminf((float)(kBuckets - 1) / (27.1f * temperature), 1e38f), 1e-37f);
     const float floor_k = fmaxf(by_p ? floor_0 : floor_x, by_k && !inf_top ? among : kNegInf);   // (what min-p drops counts for top-p)
     auto bucket = [&](float x) { return (int)fminf((top - x) * steps, (float)(kBuckets - 1)); };
     // Few of many: the tokens that top-k looks among, put in their order (each counts the ones before it); all the rest is done on them alone.
@@ -393,7 +397,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       }
       return true;
     };
-    auto lower_edge = [&](int step) { return top - ((float)step + 1.01f) / steps - 1e-6f * fabsf(top); };   // by more than the rounding of a bucket
+    // by more than the rounding of a bucket; the last step has no end
+    auto lower_edge = [&](int step) { return step == kBuckets - 1 ? kNegInf : top - ((float)step + 1.01f) / steps - 1e-6f * fabsf(top); };
     if (by_k && few_k && sorted(floor_k, k, 0)) return;
     // the step in which the running sum reaches `need`, behind a barrier; false: none does
     auto locate = [&](u64 need) {
@@ -420,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void sample_kernel(SampleArgs a) {
       const int B = end.bucket;
       const u64 over = end.over;
       // (every value of the step, and few others: by more than the rounding of a bucket)
-      const float wide = 1e-6f * fabsf(top), from = fmaxf(floor_k, lower_edge(B)), to = top - ((float)B - 0.01f) / steps + wide;
+      const float wide = 1e-6f * fabsf(top), from = fmaxf(floor_k, lower_edge(B)), to = B == kBuckets - 1 ? top : top - ((float)B - 0.01f) / steps + wide;
       all([&](int, float (&v)[VEC]) {
         if (!any(v, [&](float x) { return x >= from && x <= to; })) return;
 #pragma unroll
